@@ -258,10 +258,11 @@ def _plain_logprobs(s):
     e = torch.exp(z - m)
     l = e.sum(1, keepdim=True)
     lse = m + torch.log(l)
+    stats = torch.cat([m, torch.log(l)], 1)
     entropy = (torch.log(l) - (e * (z - m)).sum(1, keepdim=True) / l)[:, 0]
     has = s["labels"] >= 0
     at = s["labels"].clamp(min=0).long()[:, None]
-    out = {"lse": lse[:, 0], "logp": torch.where(has, (torch.gather(z, 1, at) - lse)[:, 0], 0.0), "entropy": entropy}
+    out = {"stats": stats, "logp": torch.where(has, (torch.gather(z, 1, at) - lse)[:, 0], 0.0), "entropy": entropy}
     if case["top"]:
         v, i = torch.sort(z, dim=1, descending=True, stable=True)     # equal values: the lowest class first
         out["top_idx"], out["top_logp"] = i[:, : case["top"]].to(torch.int32), v[:, : case["top"]] - lse
@@ -292,7 +293,7 @@ def _plain_attention(s):
     bucket = None if s["buckets"] is None else s["buckets"].long()
     by_row = lambda x, how="sum", start=0.0: torch.segment_reduce(x, how, offsets=ptr, axis=0, initial=start)  # noqa: E731
     Y = torch.empty(n_rows, heads * dv, device=DEV)
-    lse = torch.empty(n_rows, heads, device=DEV)
+    stats = torch.empty(n_rows, heads, 2, device=DEV)
     train = case["train"]
     if train:
         order, t_ptr = s["t_order"].long(), s["t_ptr"].long()
@@ -312,7 +313,7 @@ def _plain_attention(s):
         m = by_row(x, "max", -math.inf)
         e = torch.exp(x - m[row])
         l = by_row(e)
-        lse[:, h] = m + torch.log(l)
+        stats[:, h, 0], stats[:, h, 1] = m, torch.log(l)
         alpha = e / l[row]
         keep = (_keep(s, row, col, h).float() / (1.0 - p)) if p > 0.0 else None
         w = alpha if keep is None else alpha * keep
@@ -332,7 +333,7 @@ def _plain_attention(s):
             ds = (dt * slope * s["scale"])[:, None]
             dQ[:, h * d:(h + 1) * d] = by_row(ds * k[col])
             dK[:, g * d:(g + 1) * d] += by_col(ds * q[row])
-    out = {"Y": Y.to(dtype), "lse": lse}
+    out = {"Y": Y.to(dtype), "stats": stats}
     if train:
         out.update(dQ=dQ.to(dtype), dK=dK.to(dtype), dV=dV.to(dtype))
         if dbias is not None:
@@ -351,18 +352,18 @@ def run(s):
         return {"Y": ctx.dropout(s["X"], case["p"], s["drop_seed"], s["offset"], add=s["add"])}
     if case["op"] == "logprobs":
         r = ctx.logprobs(s["Z"], s["labels"], top=case["top"])
-        out = {"lse": r.lse, "logp": r.logp, "entropy": r.entropy}
+        out = {"stats": r.stats, "logp": r.logp, "entropy": r.entropy}
         if case["top"]:
             out["top_idx"], out["top_logp"] = r.top_idx, r.top_logp
         if case["train"]:
-            out["dZ"] = ctx.logprobs_backward(s["Z"], s["labels"], r.lse, g_logp=s["g_logp"], entropy=r.entropy, g_entropy=s["g_entropy"])
+            out["dZ"] = ctx.logprobs_backward(s["Z"], s["labels"], r.stats, g_logp=s["g_logp"], entropy=r.entropy, g_entropy=s["g_entropy"])
         return out
     opts = dict(n_kv_heads=case["kv_heads"], scale=s["scale"], cap=case["cap"], buckets=s["buckets"], bias=s["bias"], p=case["p"], seed=s["drop_seed"],
                 offset=s["offset"])
-    Y, lse = ctx.attention(s["A"], s["Q"], s["K"], s["V"], case["heads"], **opts)
-    out = {"Y": Y, "lse": lse}
+    Y, stats = ctx.attention(s["A"], s["Q"], s["K"], s["V"], case["heads"], **opts)
+    out = {"Y": Y, "stats": stats}
     if case["train"]:
-        dQ, dK, dV, dbias = ctx.attention_backward(s["A"], s["At"], s["t_pos"], s["Q"], s["K"], s["V"], case["heads"], Y, lse, s["dY"], **opts)
+        dQ, dK, dV, dbias = ctx.attention_backward(s["A"], s["At"], s["t_pos"], s["Q"], s["K"], s["V"], case["heads"], Y, stats, s["dY"], **opts)
         out.update(dQ=dQ, dK=dK, dV=dV)
         if dbias is not None:
             out["dbias"] = dbias
@@ -417,7 +418,8 @@ def _exact_logprobs(s):
         i = torch.arange(z.size(0), device=DEV)
         has = (lab >= 0).double()
         ent = -(p * lp).sum(1)
-        got = {"lse": (z - lp)[:, 0], "logp": lp[i, lab.clamp(min=0)] * has, "entropy": ent}
+        top = z.amax(1)
+        got = {"stats": torch.stack([top, (z - lp)[:, 0] - top], 1), "logp": lp[i, lab.clamp(min=0)] * has, "entropy": ent}
         if case["top"]:
             # order by value, then by class from the lowest: one whole number for both
             bits = s["Z"][lo:lo + per].float().view(torch.int32).long()
@@ -445,7 +447,7 @@ def _exact_attention(s):
     if nnz * heads * max(d, dv) > 12_000_000_000:
         return None
     new = lambda *shape: torch.zeros(shape, dtype=torch.float64, device=DEV)  # noqa: E731
-    Y, lse = new(n_rows, heads, dv), new(n_rows, heads)
+    Y, stats = new(n_rows, heads, dv), new(n_rows, heads, 2)
     dQ, dK, dV, dbias = new(n_rows, heads, d), new(n_cols, kv, d), new(n_cols, kv, dv), new(heads, max(1, case["buckets"]))
     row = torch.searchsorted(s["row_ptr"].long(), torch.arange(nnz, device=DEV), right=True) - 1
     col = s["col_idx"].long()
@@ -461,8 +463,8 @@ def _exact_attention(s):
             x = x + s["bias"][h].double()[s["buckets"].long()]
         top = torch.full((n_rows,), -math.inf, dtype=torch.float64, device=DEV).scatter_reduce_(0, row, x, "amax")
         z = new(n_rows).index_add_(0, row, torch.exp(x - top[row]))
-        lse[:, h] = top + torch.log(z)
-        a = torch.exp(x - lse[row, h])
+        stats[:, h] = torch.stack([top, torch.log(z)], 1)
+        a = torch.exp(x - stats[:, h].sum(1)[row])
         kept = torch.ones_like(a)
         if p > 0.0:
             zero = torch.zeros_like(row)
@@ -483,7 +485,7 @@ def _exact_attention(s):
             dQ[:, h].index_add_(0, row[e], ds[e, None] * k[col[e]])
             dK[:, g].index_add_(0, col[e], ds[e, None] * q[row[e]])
             dV[:, g].index_add_(0, col[e], (a[e] * kept[e])[:, None] * dy[row[e]])
-    out = {"Y": Y.flatten(1), "lse": lse}
+    out = {"Y": Y.flatten(1), "stats": stats}
     if case["train"]:
         out.update(dQ=dQ.flatten(1), dK=dK.flatten(1), dV=dV.flatten(1))
         if s["bias"] is not None:
