@@ -64,6 +64,16 @@ typedef struct {
     int64_t rows, cols, ld;
 } sensei_mat;
 
+/* Element types of the operators that take a sensei_tmat (dropout, attention over a pattern, log probabilities): they compute in fp32 and round
+ * once, to nearest with ties to even, where a result is stored.  Rows may begin at any element: no leading dimension or width is slower for
+ * its alignment alone. */
+enum { SENSEI_F32 = 0, SENSEI_BF16 = 1, SENSEI_F16 = 2 };
+typedef struct {
+    const void *ptr; /* device */
+    int64_t rows, cols, ld;
+    int type;        /* SENSEI_F32, SENSEI_BF16, SENSEI_F16 */
+} sensei_tmat;
+
 enum { SENSEI_ACT_NONE = 0, SENSEI_ACT_RELU = 1 };
 enum { SENSEI_KIND_GCN = 0, SENSEI_KIND_GAT = 1 };
 
@@ -474,6 +484,87 @@ int sensei_gat_attention_path(const sensei_csr *A, int f_in, int f_out, int n_he
 int sensei_gat_layer_heads(sensei_ctx *ctx, const sensei_csr *A, sensei_mat X, sensei_mat W, const float *a_l, const float *a_r,
                            int n_heads, float neg_slope, float *Y, int64_t ldy, int activation, int comp_id, void *workspace,
                            size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------- around the layers of a training step (not steps of the paper's method) */
+
+/* Dropout: Y = add + keep (x) X / (1 - p), 0 <= p < 1; `add` may be NULL (no residual).  Element (i, c) is kept if word c % 4 of
+ * Philox4x32 with seven rounds (Salmon et al. 2011) at counter (c / 4, i, 0, offset) under the key `seed` (low word, high word) is at
+ * least p 2^32 rounded to the nearest integer.  The mask is a function of seed, offset and the element's place alone: it is never stored,
+ * the backward pass is the same call on dY (without add), and any part of a mask can be formed again.  Use another offset for every layer and
+ * step under one seed.  offset_dev: NULL, or a device word that is added to offset (modulo 2^32) when the kernel runs, so that a captured graph
+ * draws another mask at every replay once the program advances it.
+ * X, add and Y share a type; Y: X.rows x X.cols, ldy.  Y may be X or add itself (same pointer and leading dimension), otherwise it must not
+ * overlap them.  A dropped element is 0 whatever X holds there.  At most 2^32 - 1 rows and 2^30 columns. */
+int sensei_dropout(sensei_ctx *ctx, sensei_tmat X, const sensei_tmat *add, double p, uint64_t seed, uint32_t offset, const uint32_t *offset_dev,
+                   void *Y, int64_t ldy, void *stream);
+
+/* Multi-head attention over the stored entries of a pattern (key-query attention as in sensei_dotgat_layer, on projections the caller formed):
+ * query head h (d_k columns [h d_k, (h + 1) d_k) of Q) attends with key head g = h n_kv_heads / n_heads of K and V,
+ *     s_ij = scale <Q_i^h, K_j^g>,  s_ij <- cap tanh(s_ij / cap) if cap > 0,  t_ij = s_ij + bias[h, bucket_ij],
+ *     alpha_i = softmax of t over the entries of row i,  Y_i^h = sum_j drop(alpha_ij) V_j^g.
+ * The pattern is the mask: a block-diagonal one keeps the graphs (or documents) of a batch apart, a banded or triangular one limits the
+ * distance or the direction, sampled neighbours are a rectangular one.  bucket: nnz bytes (device, in the pattern's order) that sort the
+ * entries by distance or kind (a number from n_buckets on counts as the last bucket), bias: n_heads x n_buckets floats (device); n_buckets = 0: no
+ * bias, both ignored.  bias may be -inf: such entries are masked and have no share, whatever Q, K or V hold; K and V of other entries enter as
+ * they are (an infinity or NaN there comes out in the rows that attend to it).  drop: alpha_ij keep / (1 - p), the softmax's sum over all
+ * entries; the weight of entry (i, j) and query head h is kept if word h % 4 of the generator of sensei_dropout at counter
+ * (j, i, 2^31 + h / 4, offset [+ *offset_dev]) is at least p 2^32: the mask does not depend on the order of the entries.
+ * A row with no entry, or with masked ones only, has Y = 0 and the pair (-inf, -inf).
+ *   Q: n_rows x n_heads d_k, K: n_cols x n_kv_heads d_k, V: n_cols x n_kv_heads d_v, one type; Y: n_rows x n_heads d_v of that type, ldy;
+ *   stats: n_rows x n_heads pairs of floats (max of t over the row, log of the sum of exp(t - max)), for the backward pass.
+ * 1 <= d_k, d_v <= 256; n_kv_heads divides n_heads <= 512; 0 <= n_buckets <= 128, n_heads n_buckets <= 8192; 0 <= p < 1; cap >= 0 and scale finite.
+ * Column panels, tile splits and values attached to the pattern are not used. */
+typedef struct {
+    int n_heads, n_kv_heads;
+    float scale, cap;         /* cap = 0: scores are not capped */
+    const uint8_t *bucket;    /* device, nnz */
+    const float *bias;        /* device, n_heads x n_buckets */
+    int n_buckets;
+    double p;                 /* share of weights that is dropped */
+    uint64_t seed;
+    uint32_t offset;
+    const uint32_t *offset_dev; /* device, or NULL */
+} sensei_attention_opts;
+#define SENSEI_MAX_HEAD_WIDTH 256
+#define SENSEI_MAX_HEADS 512
+#define SENSEI_MAX_BUCKETS 128
+int sensei_attention_workspace(const sensei_csr *A, const sensei_attention_opts *opts, int d_k, int d_v, int type, size_t *bytes);
+int sensei_attention(sensei_ctx *ctx, const sensei_csr *A, sensei_tmat Q, sensei_tmat K, sensei_tmat V, const sensei_attention_opts *opts, void *Y,
+                     int64_t ldy, float *stats, void *workspace, size_t ws_bytes, void *stream);
+
+/* Backward of sensei_attention: with keep_ij the forward's (0 or 1 / (1 - p)), alpha formed again from `stats`, D_i^h = <dY_i^h, Y_i^h>,
+ *   dt_ij = alpha_ij (keep_ij <dY_i^h, V_j^g> - D_i^h),   ds_ij = dt_ij (1 - tanh^2(s_ij / cap)) scale,
+ *   dQ_i^h = sum_j ds_ij K_j^g,   dK_j^g = sum_(h of g) sum_i ds_ij Q_i^h,   dV_j^g = sum_(h of g) sum_i alpha_ij keep_ij dY_i^h,
+ *   dbias[h, b] = sum of dt_ij over the entries of bucket b (NULL: not wanted).
+ * At: the transposed pattern (A itself when symmetric); t_pos: sensei_transpose_positions, needed with buckets only (else NULL).  opts, Q, K, V: as
+ * the forward got them; Y, stats: what it returned.  dY: n_rows x n_heads d_v, dQ, dK, dV like Q, K, V, all of their type with their own leading
+ * dimensions; dbias fp32.  Columns that no row attends to get dK = dV = 0.  Every sum has one order: results do not depend on scheduling. */
+int sensei_attention_backward_workspace(const sensei_csr *A, const sensei_attention_opts *opts, int d_k, int d_v, int type, size_t *bytes);
+int sensei_attention_backward(sensei_ctx *ctx, const sensei_csr *A, const sensei_csr *At, const int32_t *t_pos, sensei_tmat Q, sensei_tmat K, sensei_tmat V,
+                              const sensei_attention_opts *opts, sensei_tmat Y, const float *stats, sensei_tmat dY, void *dQ, int64_t lddq, void *dK,
+                              int64_t lddk, void *dV, int64_t lddv, float *dbias, void *workspace, size_t ws_bytes, void *stream);
+
+/* Log probabilities of given classes over rows of logits Z (n x classes): with lse_i = log sum_j exp(Z_ij), log p_ij = Z_ij - lse_i,
+ *   logp[i]    = log p of class labels[i] (device int32; a label outside [0, classes), such as -1, means none: 0),
+ *   entropy[i] = - sum_j p_ij log p_ij,
+ *   top_idx, top_logp: the `top` most probable classes of the row (n x top, classes from the most probable on; equal logits rank the lower class
+ *                first, a NaN ranks above every number) and their log probabilities; 0 <= top <= SENSEI_MAX_TOP, top <= classes,
+ *   stats[i]   = (max_j Z_ij, log sum_j exp(Z_ij - max)): lse is their sum; the backward takes the pair, which stays exact where the largest
+ *                logit is far from 0.
+ * Every output may be NULL (labels too without logp).  Logits of -inf mask their classes: no share in any sum, log p = -inf; a row of nothing else
+ * has logp = top_logp = -inf, entropy 0 and the pair (-inf, -inf).  A row that holds a NaN or +inf has NaN in logp, entropy and top_logp.
+ * Z is read once; long rows that are few are shared by several workgroups, for which the workspace is used (0 bytes otherwise: it may be NULL). */
+#define SENSEI_MAX_TOP 64
+int sensei_logprobs_workspace(int64_t rows, int64_t classes, int top, int type, size_t *bytes);
+int sensei_logprobs(sensei_ctx *ctx, sensei_tmat Z, const int32_t *labels, int top, float *stats, float *logp, float *entropy, int32_t *top_idx,
+                    float *top_logp, void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradient of sensei_logprobs by the chain rule: with g = g_logp[i] = dL/dlogp (NULL: none; counts only where labels[i] is a class) and
+ * h = g_entropy[i] = dL/dentropy (NULL: none; needs the forward's entropy),
+ *   dZ_ij = g ([j = labels[i]] - p_ij) - h p_ij (log p_ij + entropy_i),
+ * of Z's type, lddz.  A negative log likelihood averaged over m rows has g = -1 / m.  dZ may be Z itself (same pointer and leading dimension). */
+int sensei_logprobs_backward(sensei_ctx *ctx, sensei_tmat Z, const int32_t *labels, const float *stats, const float *g_logp, const float *entropy,
+                             const float *g_entropy, void *dZ, int64_t lddz, void *stream);
 
 /* --------------------------------------------------------------------- selector */
 

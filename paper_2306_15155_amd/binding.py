@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -33,6 +34,8 @@ EXPORTS = (
     "sensei_panels_tune", "sensei_gcn_backward_workspace", "sensei_gcn_backward", "sensei_select_gcn_backward", "sensei_select_khop_backward", "sensei_transpose_positions",
     "sensei_gat_backward_workspace", "sensei_gat_backward", "sensei_gat_backward_heads_workspace", "sensei_gat_backward_heads", "sensei_gat_layer_heads", "sensei_sgc_workspace", "sensei_sgc_layer", "sensei_sgc_backward_workspace", "sensei_sgc_backward", "sensei_tagcn_workspace", "sensei_tagcn_layer", "sensei_tagcn_backward_workspace", "sensei_tagcn_backward", "sensei_gatv2_workspace", "sensei_gatv2_layer", "sensei_gatv2_backward_workspace", "sensei_gatv2_backward", "sensei_dotgat_workspace", "sensei_dotgat_layer", "sensei_dotgat_backward_workspace", "sensei_dotgat_backward", "sensei_tiles_remainder_panels", "sensei_tiles_bytes", "sensei_tiles_create", "sensei_tiles_info",
            "sensei_tiles_set_min_width", "sensei_tiles_destroy",
+    "sensei_dropout", "sensei_attention_workspace", "sensei_attention", "sensei_attention_backward_workspace", "sensei_attention_backward",
+    "sensei_logprobs_workspace", "sensei_logprobs", "sensei_logprobs_backward",
 )
 
 
@@ -50,6 +53,16 @@ class CsrStruct(ctypes.Structure):
 
 class MatStruct(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64)]
+
+
+class TMatStruct(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
+class AttentionOpts(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("bucket", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("n_buckets", ctypes.c_int), ("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint32),
+                ("offset_dev", ctypes.c_void_p)]
 
 
 _lib = None
@@ -140,6 +153,15 @@ def lib():
         L.sensei_panels_tune.argtypes = [vp, P(CsrStruct), vp, sz, vp, P(ctypes.c_int), P(ctypes.c_int), P(f32)]
         L.sensei_profile_enable.argtypes = [vp, i32]
         L.sensei_profile_read.argtypes = [vp, i32, P(f32), i32, P(ctypes.c_int)]
+        L.sensei_dropout.argtypes = [vp, TMatStruct, P(TMatStruct), ctypes.c_double, ctypes.c_uint64, ctypes.c_uint32, vp, vp, i64, vp]
+        L.sensei_attention_workspace.argtypes = [P(CsrStruct), P(AttentionOpts), i32, i32, i32, P(sz)]
+        L.sensei_attention.argtypes = [vp, P(CsrStruct), TMatStruct, TMatStruct, TMatStruct, P(AttentionOpts), vp, i64, vp, vp, sz, vp]
+        L.sensei_attention_backward_workspace.argtypes = [P(CsrStruct), P(AttentionOpts), i32, i32, i32, P(sz)]
+        L.sensei_attention_backward.argtypes = [vp, P(CsrStruct), P(CsrStruct), vp, TMatStruct, TMatStruct, TMatStruct, P(AttentionOpts), TMatStruct, vp, TMatStruct,
+                                                vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.sensei_logprobs_workspace.argtypes = [i64, i64, i32, i32, P(sz)]
+        L.sensei_logprobs.argtypes = [vp, TMatStruct, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.sensei_logprobs_backward.argtypes = [vp, TMatStruct, vp, vp, vp, vp, vp, vp, i64, vp]
         for name in EXPORTS:
             if name not in ("sensei_composition_name", "sensei_status_string"):
                 getattr(L, name).restype = ctypes.c_int
@@ -312,6 +334,27 @@ def _ld(t: torch.Tensor) -> int:
     return ld if rows > 1 else max(ld, cols)
 
 
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def tmat_struct(t: torch.Tensor) -> TMatStruct:
+    """A two-dimensional fp32, bf16 or fp16 tensor with its columns side by side."""
+    assert t.dtype in _TYPES and t.dim() == 2, "a matrix of fp32, bf16 or fp16"
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    assert step == 1 or cols <= 1, "columns side by side"
+    return TMatStruct(t.data_ptr(), rows, cols, ld if rows > 1 else max(ld, cols), _TYPES[t.dtype])
+
+
+class LogProbs(NamedTuple):
+    """Of every row: (max, log of the sum of exp(z - max)); log probability of its label; entropy; the most probable classes and their log
+    probabilities.  None where not asked for."""
+    stats: torch.Tensor
+    logp: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    top_idx: Optional[torch.Tensor]
+    top_logp: Optional[torch.Tensor]
+
+
 class Workspace:
     """A grow-only device byte buffer (PyTorch owns the memory)."""
 
@@ -417,6 +460,121 @@ class Context:
         _check(lib().sensei_edge_softmax(self._h, ctypes.byref(A), _ptr(e), _ptr(alpha), self.ws.ptr, self.ws.nbytes, _stream()),
                "sensei_edge_softmax")
         return alpha
+
+    # ---- around the layers: dropout, attention on given projections, log probabilities (fp32, bf16, fp16)
+    def _here(self, *tensors):
+        for t in tensors:
+            assert t is None or t.device == self.device, f"a tensor on {t.device}, the context is on {self.device}"
+
+    def _stream(self):
+        """The current stream of the context's device, which need not be the current device."""
+        return _raw_stream(self.device.index) if _raw_stream else torch.cuda.current_stream(self.device).cuda_stream
+
+    def _vector(self, t, n, dtype):
+        assert t is None or (t.dtype == dtype and t.is_contiguous() and t.numel() == n), f"{n} contiguous {dtype} values"
+
+    def _scratch(self, need):
+        """Workspace of one call from torch's allocator, which keeps calls on several streams, and captured graphs, apart."""
+        return torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+
+    def dropout(self, X, p, seed, offset=0, add=None, offset_dev=None, out=None):
+        """sensei_dropout: add + keep X / (1 - p).  The backward pass is the same call on the gradient of the result (without ``add``).  ``out`` may be
+        X or ``add``.  offset_dev: a device tensor of one int32 that is added to ``offset`` when the kernel runs."""
+        Y = torch.empty(X.shape, dtype=X.dtype, device=X.device) if out is None else out
+        self._here(X, add, offset_dev, Y)
+        self._vector(offset_dev, 1, torch.int32)
+        assert Y.shape == X.shape and Y.dtype == X.dtype
+        y = tmat_struct(Y)
+        _check(lib().sensei_dropout(self._h, tmat_struct(X), None if add is None else ctypes.byref(tmat_struct(add)), p, seed & (2 ** 64 - 1),
+                                    offset & (2 ** 32 - 1), _ptr(offset_dev), y.ptr, y.ld, self._stream()), "sensei_dropout")
+        return Y
+
+    def _attention_opts(self, A, Q, K, n_heads, n_kv_heads, scale, cap, buckets, bias, p, seed, offset, offset_dev):
+        assert (buckets is None) == (bias is None), "buckets and their bias come together"
+        n_buckets = 0
+        if bias is not None:
+            assert bias.dim() == 2 and bias.size(0) == n_heads, "a row of the bias for every head"
+            n_buckets = bias.size(1)
+            assert n_buckets >= 1
+            self._vector(bias, n_heads * n_buckets, torch.float32)
+            self._vector(buckets, A.nnz, torch.uint8)
+        self._here(buckets, bias, offset_dev)
+        self._vector(offset_dev, 1, torch.int32)
+        if scale is None:
+            scale = (Q.size(1) // n_heads) ** -0.5
+        return AttentionOpts(n_heads, n_heads if n_kv_heads is None else n_kv_heads, scale, cap, _ptr(buckets), _ptr(bias), n_buckets, p,
+                             seed & (2 ** 64 - 1), offset & (2 ** 32 - 1), _ptr(offset_dev))
+
+    def attention(self, A: CsrStruct, Q, K, V, n_heads, n_kv_heads=None, scale=None, cap=0.0, buckets=None, bias=None, p=0.0, seed=0, offset=0,
+                  offset_dev=None, out=None):
+        """sensei_attention -> (Y, stats): multi-head attention of the rows over the stored entries.  scale: 1 / sqrt(d_k) unless given; cap > 0
+        caps the scores by a tanh; bias[h, buckets[entry]] is added to them; p of the weights are dropped.  stats (n_rows, n_heads, 2) is for
+        attention_backward."""
+        o = self._attention_opts(A, Q, K, n_heads, n_kv_heads, scale, cap, buckets, bias, p, seed, offset, offset_dev)
+        q, k, v = tmat_struct(Q), tmat_struct(K), tmat_struct(V)
+        d_k, d_v = Q.size(1) // n_heads, V.size(1) // max(o.n_kv_heads, 1)
+        Y = torch.empty((A.n_rows, n_heads * d_v), dtype=Q.dtype, device=self.device) if out is None else out
+        stats = torch.empty((A.n_rows, n_heads, 2), dtype=torch.float32, device=self.device)
+        self._here(Q, K, V, Y)
+        y = tmat_struct(Y)
+        assert Y.dtype == Q.dtype and Y.shape == (A.n_rows, n_heads * d_v)
+        need = ctypes.c_size_t()
+        _check(lib().sensei_attention_workspace(ctypes.byref(A), ctypes.byref(o), d_k, d_v, q.type, ctypes.byref(need)), "sensei_attention_workspace")
+        ws = self._scratch(need)
+        _check(lib().sensei_attention(self._h, ctypes.byref(A), q, k, v, ctypes.byref(o), y.ptr, y.ld, _ptr(stats), _ptr(ws), need.value,
+                                      self._stream()), "sensei_attention")
+        return Y, stats
+
+    def attention_backward(self, A: CsrStruct, At: CsrStruct, t_pos, Q, K, V, n_heads, Y, stats, dY, n_kv_heads=None, scale=None, cap=0.0, buckets=None,
+                           bias=None, p=0.0, seed=0, offset=0, offset_dev=None, want_dbias=True):
+        """Backward of attention -> (dQ, dK, dV, dbias or None), with the arguments the forward had and what it returned.  t_pos
+        (transpose_positions) is needed with buckets only."""
+        o = self._attention_opts(A, Q, K, n_heads, n_kv_heads, scale, cap, buckets, bias, p, seed, offset, offset_dev)
+        q, k, v, y, dy = (tmat_struct(t) for t in (Q, K, V, Y, dY))
+        d_k, d_v = Q.size(1) // n_heads, V.size(1) // max(o.n_kv_heads, 1)
+        self._here(Q, K, V, Y, dY, stats, t_pos)
+        self._vector(stats, A.n_rows * n_heads * 2, torch.float32)
+        assert t_pos is None or (t_pos.dtype == torch.int32 and t_pos.is_contiguous() and t_pos.numel() >= A.nnz)
+        dQ, dK, dV = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (Q, K, V))
+        dbias = torch.empty_like(bias) if bias is not None and want_dbias else None
+        need = ctypes.c_size_t()
+        _check(lib().sensei_attention_backward_workspace(ctypes.byref(A), ctypes.byref(o), d_k, d_v, q.type, ctypes.byref(need)),
+               "sensei_attention_backward_workspace")
+        ws = self._scratch(need)
+        _check(lib().sensei_attention_backward(self._h, ctypes.byref(A), ctypes.byref(At), _ptr(t_pos), q, k, v, ctypes.byref(o), y, _ptr(stats), dy, _ptr(dQ),
+                                               tmat_struct(dQ).ld, _ptr(dK), tmat_struct(dK).ld, _ptr(dV), tmat_struct(dV).ld, _ptr(dbias), _ptr(ws),
+                                               need.value, self._stream()), "sensei_attention_backward")
+        return dQ, dK, dV, dbias
+
+    def logprobs(self, Z, labels=None, top=0, entropy=True) -> LogProbs:
+        """sensei_logprobs of the rows of Z: log probability of labels (int32, outside the classes: none), entropy, the ``top`` most probable classes."""
+        n, z = Z.size(0), tmat_struct(Z)
+        self._here(Z, labels)
+        self._vector(labels, n, torch.int32)
+        new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=self.device)  # noqa: E731
+        r = LogProbs(new(n, 2), None if labels is None else new(n), new(n) if entropy else None,
+                     torch.empty((n, top), dtype=torch.int32, device=self.device) if top > 0 else None, new(n, top) if top > 0 else None)
+        need = ctypes.c_size_t()
+        _check(lib().sensei_logprobs_workspace(n, Z.size(1), top, z.type, ctypes.byref(need)), "sensei_logprobs_workspace")
+        ws = self._scratch(need)
+        _check(lib().sensei_logprobs(self._h, z, _ptr(labels), top, _ptr(r.stats), _ptr(r.logp), _ptr(r.entropy), _ptr(r.top_idx), _ptr(r.top_logp),
+                                     _ptr(ws), need.value, self._stream()), "sensei_logprobs")
+        return r
+
+    def logprobs_backward(self, Z, labels, stats, g_logp=None, entropy=None, g_entropy=None, out=None):
+        """Gradient of logprobs -> dZ from the gradients of the rows' log probability and entropy (either may be None); ``out`` may be Z."""
+        n = Z.size(0)
+        dZ = torch.empty(Z.shape, dtype=Z.dtype, device=Z.device) if out is None else out
+        self._here(Z, labels, stats, g_logp, entropy, g_entropy, dZ)
+        self._vector(labels, n, torch.int32)
+        self._vector(stats, 2 * n, torch.float32)
+        for t in (g_logp, entropy, g_entropy):
+            self._vector(t, n, torch.float32)
+        assert dZ.shape == Z.shape and dZ.dtype == Z.dtype
+        d = tmat_struct(dZ)
+        _check(lib().sensei_logprobs_backward(self._h, tmat_struct(Z), _ptr(labels), _ptr(stats), _ptr(g_logp), _ptr(entropy), _ptr(g_entropy), d.ptr, d.ld,
+                                              self._stream()), "sensei_logprobs_backward")
+        return dZ
 
     # ---- layers
     def gcn_workspace(self, A: CsrStruct, f_in, f_out, comp_id) -> int:

@@ -1786,6 +1786,72 @@ size_t select_scratch_bytes(int kind, const sensei_csr &A, int f_in, int f_out) 
     return b + layer + 1024;
 }
 
+// ---- checks of the operators on fp32, bf16 and fp16 matrices
+
+size_t elem_bytes(int type) { return type == SENSEI_F32 ? 4 : 2; }
+bool tmat_ok(const sensei_tmat &M) {
+    return M.rows >= 0 && M.cols >= 0 && M.ld >= M.cols && M.type >= SENSEI_F32 && M.type <= SENSEI_F16 && (M.ptr || M.rows == 0 || M.cols == 0) &&
+           reinterpret_cast<uintptr_t>(M.ptr) % elem_bytes(M.type) == 0;
+}
+struct Span { const void *p; size_t n; };
+Span span(const void *p, int64_t rows, int64_t cols, int64_t ld, int type) {
+    return {p, rows <= 0 || cols <= 0 ? 0 : (size_t)((rows - 1) * ld + cols) * elem_bytes(type)};
+}
+Span span(const sensei_tmat &M) { return span(M.ptr, M.rows, M.cols, M.ld, M.type); }
+bool meet(const Span &a, const Span &b) { return overlap(a.p, a.n, b.p, b.n); }
+// no output meets another or an input; neither meets the workspace
+template <size_t NO, size_t NI> bool apart(const Span (&outs)[NO], const Span (&ins)[NI], const Span &ws) {
+    for (size_t a = 0; a < NO; ++a) {
+        if (meet(outs[a], ws)) return false;
+        for (const Span &i : ins)
+            if (meet(outs[a], i)) return false;
+        for (size_t b = a + 1; b < NO; ++b)
+            if (meet(outs[a], outs[b])) return false;
+    }
+    for (const Span &i : ins)
+        if (meet(i, ws)) return false;
+    return true;
+}
+
+// The context's device for the length of a call, whichever was current before it.
+struct OnDevice {
+    int before = -1;
+    bool ok;
+    explicit OnDevice(int device) {
+        int now = 0;
+        ok = hipGetDevice(&now) == hipSuccess;
+        if (ok && now != device) {
+            ok = hipSetDevice(device) == hipSuccess;
+            if (ok) before = now;
+        }
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+bool attention_opts_ok(const sensei_attention_opts *o, int64_t d_k, int64_t d_v) {
+    return o && o->n_heads >= 1 && o->n_heads <= SENSEI_MAX_HEADS && o->n_kv_heads >= 1 && o->n_heads % o->n_kv_heads == 0 && d_k >= 1 && d_v >= 1 &&
+           d_k <= SENSEI_MAX_HEAD_WIDTH && d_v <= SENSEI_MAX_HEAD_WIDTH && o->n_buckets >= 0 && o->n_buckets <= SENSEI_MAX_BUCKETS &&
+           (int64_t)o->n_heads * o->n_buckets <= 8192 && std::isfinite(o->scale) && std::isfinite(o->cap) && o->cap >= 0.f && o->p >= 0.0 && o->p < 1.0;
+}
+AttentionCall attention_call(const sensei_csr *A, const sensei_attention_opts &o, int d_k, int d_v, int type) {
+    AttentionCall c = {};
+    c.A = A;
+    c.heads = o.n_heads; c.kv_heads = o.n_kv_heads; c.d = d_k; c.dv = d_v; c.type = type; c.elem = (int)elem_bytes(type);
+    c.scale = o.scale; c.cap = o.cap; c.bucket = o.bucket; c.bias = o.bias; c.n_buckets = o.n_buckets;
+    c.p = o.p; c.seed = o.seed; c.offset = o.offset; c.offset_dev = o.offset_dev;
+    return c;
+}
+// operands that both directions take
+bool attention_operands_ok(const sensei_csr *A, const sensei_tmat &Q, const sensei_tmat &K, const sensei_tmat &V, const sensei_attention_opts *o) {
+    if (!csr_ok(A, false) || !o || o->n_heads < 1 || o->n_kv_heads < 1 || !tmat_ok(Q) || !tmat_ok(K) || !tmat_ok(V)) return false;
+    if (Q.type != K.type || Q.type != V.type || Q.rows != A->n_rows || K.rows != A->n_cols || V.rows != A->n_cols) return false;
+    if (Q.cols % o->n_heads || K.cols % o->n_kv_heads || V.cols % o->n_kv_heads || Q.cols / o->n_heads != K.cols / o->n_kv_heads) return false;
+    if (!attention_opts_ok(o, Q.cols / o->n_heads, V.cols / o->n_kv_heads)) return false;
+    return o->n_buckets == 0 || (o->bias && (o->bucket || A->nnz == 0));
+}
+
 }  // namespace
 
 // ------------------------------------------------------------------- C ABI
@@ -2962,6 +3028,132 @@ int sensei_dotgat_backward(sensei_ctx *ctx, const sensei_csr *A, const sensei_cs
     }
     return run_dotgat_backward(*A, *At, t_pos, X, W_q, W_k, W_v, scale, Y, ldy, dY, activation, dX, lddx, dW_q, lddwq, dW_k, lddwk, dW_v, lddwv,
                                workspace, ws_bytes, as_stream(stream));
+}
+
+// ---- dropout, attention over a pattern, log probabilities
+
+int sensei_dropout(sensei_ctx *ctx, sensei_tmat X, const sensei_tmat *add, double p, uint64_t seed, uint32_t offset, const uint32_t *offset_dev,
+                   void *Y, int64_t ldy, void *stream) {
+    if (!ctx || !tmat_ok(X) || ldy < X.cols || !(p >= 0.0 && p < 1.0)) return SENSEI_INVALID_ARGUMENT;
+    if (X.rows > 0xFFFFFFFFll || X.cols > (1 << 30)) return SENSEI_INVALID_ARGUMENT;
+    if (X.rows > 0 && X.cols > 0 && (!Y || reinterpret_cast<uintptr_t>(Y) % elem_bytes(X.type))) return SENSEI_INVALID_ARGUMENT;
+    if (add && (!tmat_ok(*add) || add->type != X.type || add->rows != X.rows || add->cols != X.cols)) return SENSEI_INVALID_ARGUMENT;
+    const Span y = span(Y, X.rows, X.cols, ldy, X.type);
+    if (Y == X.ptr ? ldy != X.ld : meet(y, span(X))) return SENSEI_INVALID_ARGUMENT;
+    if (add && (Y == add->ptr ? ldy != add->ld : meet(y, span(*add)))) return SENSEI_INVALID_ARGUMENT;
+    if (X.rows == 0 || X.cols == 0) return SENSEI_OK;
+    OnDevice on(ctx->device);
+    if (!on.ok) return SENSEI_HIP_ERROR;
+    return hip_status(launch_dropout(X, add, p, seed, offset, offset_dev, Y, ldy, as_stream(stream)));
+}
+
+int sensei_attention_workspace(const sensei_csr *A, const sensei_attention_opts *opts, int d_k, int d_v, int type, size_t *bytes) {
+    if (!csr_ok(A, false) || !attention_opts_ok(opts, d_k, d_v) || type < SENSEI_F32 || type > SENSEI_F16 || !bytes) return SENSEI_INVALID_ARGUMENT;
+    *bytes = attention_ws_bytes(attention_call(A, *opts, d_k, d_v, type));
+    return SENSEI_OK;
+}
+
+int sensei_attention(sensei_ctx *ctx, const sensei_csr *A, sensei_tmat Q, sensei_tmat K, sensei_tmat V, const sensei_attention_opts *opts, void *Y,
+                     int64_t ldy, float *stats, void *workspace, size_t ws_bytes, void *stream) {
+    if (!ctx || !attention_operands_ok(A, Q, K, V, opts)) return SENSEI_INVALID_ARGUMENT;
+    const int d_k = (int)(Q.cols / opts->n_heads), d_v = (int)(V.cols / opts->n_kv_heads);
+    const int64_t width = (int64_t)opts->n_heads * d_v;
+    if (ldy < width || !workspace || reinterpret_cast<uintptr_t>(workspace) % 256) return SENSEI_INVALID_ARGUMENT;
+    if (A->n_rows > 0 && (!Y || !stats || reinterpret_cast<uintptr_t>(Y) % elem_bytes(Q.type) || reinterpret_cast<uintptr_t>(stats) % 8)) return SENSEI_INVALID_ARGUMENT;
+    const Span outs[] = {span(Y, A->n_rows, width, ldy, Q.type), {stats, (size_t)A->n_rows * opts->n_heads * 8}};
+    const Span ins[] = {span(Q), span(K), span(V), {opts->n_buckets ? opts->bucket : nullptr, (size_t)A->nnz}, {opts->n_buckets ? opts->bias : nullptr, (size_t)opts->n_heads * opts->n_buckets * 4}};
+    if (!apart(outs, ins, Span{workspace, ws_bytes})) return SENSEI_INVALID_ARGUMENT;
+    AttentionCall c = attention_call(A, *opts, d_k, d_v, Q.type);
+    if (ws_bytes < attention_ws_bytes(c)) return SENSEI_WORKSPACE_TOO_SMALL;
+    if (A->n_rows == 0) return SENSEI_OK;
+    OnDevice on(ctx->device);
+    if (!on.ok) return SENSEI_HIP_ERROR;
+    c.Q = Q.ptr; c.K = K.ptr; c.V = V.ptr; c.ldq = Q.ld; c.ldk = K.ld; c.ldv = V.ld;
+    c.out = Y; c.ldo = ldy;
+    c.stats = reinterpret_cast<float2 *>(stats);
+    return hip_status(launch_attention(c, static_cast<char *>(workspace), as_stream(stream)));
+}
+
+int sensei_attention_backward_workspace(const sensei_csr *A, const sensei_attention_opts *opts, int d_k, int d_v, int type, size_t *bytes) {
+    if (!csr_ok(A, false) || !attention_opts_ok(opts, d_k, d_v) || type < SENSEI_F32 || type > SENSEI_F16 || !bytes) return SENSEI_INVALID_ARGUMENT;
+    AttentionCall c = attention_call(A, *opts, d_k, d_v, type);
+    float with_gradient;
+    c.dbias = &with_gradient;   // room for it, wanted or not
+    *bytes = attention_backward_ws_bytes(c);
+    return SENSEI_OK;
+}
+
+int sensei_attention_backward(sensei_ctx *ctx, const sensei_csr *A, const sensei_csr *At, const int32_t *t_pos, sensei_tmat Q, sensei_tmat K, sensei_tmat V,
+                              const sensei_attention_opts *opts, sensei_tmat Y, const float *stats, sensei_tmat dY, void *dQ, int64_t lddq, void *dK,
+                              int64_t lddk, void *dV, int64_t lddv, float *dbias, void *workspace, size_t ws_bytes, void *stream) {
+    if (!ctx || !attention_operands_ok(A, Q, K, V, opts) || !csr_ok(At, false) || !tmat_ok(Y) || !tmat_ok(dY)) return SENSEI_INVALID_ARGUMENT;
+    if (At->n_rows != A->n_cols || At->n_cols != A->n_rows || At->nnz != A->nnz) return SENSEI_INVALID_ARGUMENT;
+    const int d_k = (int)(Q.cols / opts->n_heads), d_v = (int)(V.cols / opts->n_kv_heads);
+    const int64_t width = (int64_t)opts->n_heads * d_v;
+    if (Y.type != Q.type || dY.type != Q.type || Y.rows != A->n_rows || dY.rows != A->n_rows || Y.cols != width || dY.cols != width) return SENSEI_INVALID_ARGUMENT;
+    if (lddq < Q.cols || lddk < K.cols || lddv < V.cols || !workspace || reinterpret_cast<uintptr_t>(workspace) % 256) return SENSEI_INVALID_ARGUMENT;
+    if ((A->n_rows > 0 && (!dQ || !stats)) || (A->n_cols > 0 && (!dK || !dV))) return SENSEI_INVALID_ARGUMENT;
+    for (const void *p : {(const void *)dQ, (const void *)dK, (const void *)dV})
+        if (reinterpret_cast<uintptr_t>(p) % elem_bytes(Q.type)) return SENSEI_INVALID_ARGUMENT;
+    if (reinterpret_cast<uintptr_t>(stats) % 8) return SENSEI_INVALID_ARGUMENT;
+    if (opts->n_buckets > 0 && A->nnz > 0 && !t_pos) return SENSEI_INVALID_ARGUMENT;
+    if (opts->n_buckets == 0) dbias = nullptr;
+    const size_t table = (size_t)opts->n_heads * opts->n_buckets * 4;
+    const Span outs[] = {span(dQ, Q.rows, Q.cols, lddq, Q.type), span(dK, K.rows, K.cols, lddk, K.type), span(dV, V.rows, V.cols, lddv, V.type), {dbias, table}};
+    const Span ins[] = {span(Q), span(K), span(V), span(Y), span(dY), {stats, (size_t)A->n_rows * opts->n_heads * 8}, {opts->n_buckets ? opts->bucket : nullptr, (size_t)A->nnz},
+                        {opts->n_buckets ? opts->bias : nullptr, table}, {opts->n_buckets ? t_pos : nullptr, (size_t)A->nnz * 4}};
+    if (!apart(outs, ins, Span{workspace, ws_bytes})) return SENSEI_INVALID_ARGUMENT;
+    AttentionCall c = attention_call(A, *opts, d_k, d_v, Q.type);
+    c.dbias = dbias;
+    if (ws_bytes < attention_backward_ws_bytes(c)) return SENSEI_WORKSPACE_TOO_SMALL;
+    OnDevice on(ctx->device);
+    if (!on.ok) return SENSEI_HIP_ERROR;
+    c.At = At; c.t_pos = t_pos;
+    c.Q = Q.ptr; c.K = K.ptr; c.V = V.ptr; c.Y = Y.ptr; c.dY = dY.ptr;
+    c.ldq = Q.ld; c.ldk = K.ld; c.ldv = V.ld; c.ldy = Y.ld; c.lddy = dY.ld;
+    c.dQ = dQ; c.dK = dK; c.dV = dV; c.lddq = lddq; c.lddk = lddk; c.lddv = lddv;
+    c.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
+    return hip_status(launch_attention_backward(c, static_cast<char *>(workspace), as_stream(stream)));
+}
+
+int sensei_logprobs_workspace(int64_t rows, int64_t classes, int top, int type, size_t *bytes) {
+    if (rows < 0 || classes < 1 || classes > (1 << 30) || top < 0 || top > SENSEI_MAX_TOP || top > classes || type < SENSEI_F32 || type > SENSEI_F16 || !bytes)
+        return SENSEI_INVALID_ARGUMENT;
+    *bytes = logprobs_ws_bytes(rows, (int)classes, top, type);
+    return SENSEI_OK;
+}
+
+int sensei_logprobs(sensei_ctx *ctx, sensei_tmat Z, const int32_t *labels, int top, float *stats, float *logp, float *entropy, int32_t *top_idx,
+                    float *top_logp, void *workspace, size_t ws_bytes, void *stream) {
+    if (!ctx || !tmat_ok(Z) || Z.cols < 1 || Z.cols > (1 << 30) || top < 0 || top > SENSEI_MAX_TOP || top > Z.cols) return SENSEI_INVALID_ARGUMENT;
+    if (Z.rows > 0 && ((logp && !labels) || (top > 0 && (!top_idx || !top_logp)) || reinterpret_cast<uintptr_t>(stats) % 8)) return SENSEI_INVALID_ARGUMENT;
+    const size_t n = (size_t)Z.rows * 4, need = logprobs_ws_bytes(Z.rows, (int)Z.cols, top, Z.type);
+    const Span outs[] = {{stats, 2 * n}, {logp, n}, {entropy, n}, {top > 0 ? top_idx : nullptr, n * top}, {top > 0 ? top_logp : nullptr, n * top}};
+    const Span ins[] = {span(Z), {logp ? labels : nullptr, n}};
+    if (!apart(outs, ins, Span{workspace, ws_bytes})) return SENSEI_INVALID_ARGUMENT;
+    if (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)) return SENSEI_INVALID_ARGUMENT;
+    if (ws_bytes < need) return SENSEI_WORKSPACE_TOO_SMALL;
+    if (Z.rows == 0) return SENSEI_OK;
+    OnDevice on(ctx->device);
+    if (!on.ok) return SENSEI_HIP_ERROR;
+    return hip_status(launch_logprobs(Z, labels, top, reinterpret_cast<float2 *>(stats), logp, entropy, top_idx, top_logp, workspace, as_stream(stream)));
+}
+
+int sensei_logprobs_backward(sensei_ctx *ctx, sensei_tmat Z, const int32_t *labels, const float *stats, const float *g_logp, const float *entropy,
+                             const float *g_entropy, void *dZ, int64_t lddz, void *stream) {
+    if (!ctx || !tmat_ok(Z) || Z.cols < 1 || Z.cols > (1 << 30) || lddz < Z.cols) return SENSEI_INVALID_ARGUMENT;
+    if (Z.rows > 0 && (!stats || reinterpret_cast<uintptr_t>(stats) % 8 || !dZ || reinterpret_cast<uintptr_t>(dZ) % elem_bytes(Z.type) || (g_logp && !labels) ||
+                       (g_entropy && !entropy)))
+        return SENSEI_INVALID_ARGUMENT;
+    const size_t n = (size_t)Z.rows * 4;
+    const Span out = span(dZ, Z.rows, Z.cols, lddz, Z.type), ins[] = {{g_logp ? labels : nullptr, n}, {stats, 2 * n}, {g_logp, n}, {g_entropy ? entropy : nullptr, n}, {g_entropy, n}};
+    if (dZ == Z.ptr ? lddz != Z.ld : meet(out, span(Z))) return SENSEI_INVALID_ARGUMENT;
+    for (const Span &i : ins)
+        if (meet(out, i)) return SENSEI_INVALID_ARGUMENT;
+    if (Z.rows == 0) return SENSEI_OK;
+    OnDevice on(ctx->device);
+    if (!on.ok) return SENSEI_HIP_ERROR;
+    return hip_status(launch_logprobs_backward(Z, labels, reinterpret_cast<const float2 *>(stats), g_logp, entropy, g_entropy, dZ, lddz, as_stream(stream)));
 }
 
 int sensei_select_workspace(int kind, const sensei_csr *A, int f_in, int f_out, size_t *bytes) {

@@ -353,6 +353,47 @@ hipError_t launch_gemm_tn(const float *A, int64_t lda, const float *B, int64_t l
 hipError_t launch_transpose(const float *W, int64_t ldw, int rows, int cols, float *Wt, int64_t ldt, hipStream_t s, int count = 1, int64_t w_step = 0,
                             int64_t wt_step = 0);
 
+// ---- dropout, attention over a pattern, log probabilities of labels (fp32, bf16, fp16)
+// a word of the generator below this drops its element: p 2^32, rounded to nearest
+inline uint32_t drop_threshold(double p) {
+    const double t = __builtin_nearbyint(p * 4294967296.0);
+    return t >= 4294967295.0 ? 0xFFFFFFFFu : (uint32_t)t;
+}
+hipError_t launch_dropout(const sensei_tmat &X, const sensei_tmat *add, double p, uint64_t seed, uint32_t offset, const uint32_t *offset_dev, void *Y, int64_t ldy,
+                          hipStream_t s);
+size_t logprobs_ws_bytes(int64_t rows, int classes, int top, int type);
+// stats: (max, log of the sum of exp(z - max)) of every row
+hipError_t launch_logprobs(const sensei_tmat &Z, const int32_t *labels, int top, float2 *stats, float *logp, float *entropy, int32_t *top_idx, float *top_logp,
+                           void *workspace, hipStream_t s);
+hipError_t launch_logprobs_backward(const sensei_tmat &Z, const int32_t *labels, const float2 *stats, const float *g_logp, const float *entropy, const float *g_entropy,
+                                    void *dZ, int64_t lddz, hipStream_t s);
+
+struct AttentionCall {
+    const sensei_csr *A, *At;        // At, t_pos, Y and dY: backward only
+    const int32_t *t_pos;
+    const void *Q, *K, *V, *Y, *dY;
+    int64_t ldq, ldk, ldv, ldy, lddy;
+    void *out;                       // forward
+    int64_t ldo;
+    void *dQ, *dK, *dV;              // backward
+    int64_t lddq, lddk, lddv;
+    float *dbias;                    // may be null
+    float2 *stats;                   // n_rows x heads pairs, written by the forward
+    int heads, kv_heads, d, dv, type, elem;   // elem: bytes of an element
+    float scale, cap;
+    const uint8_t *bucket;
+    const float *bias;
+    int n_buckets;
+    double p;
+    uint64_t seed;
+    uint32_t offset;
+    const uint32_t *offset_dev;
+};
+size_t attention_ws_bytes(const AttentionCall &c);
+hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s);
+size_t attention_backward_ws_bytes(const AttentionCall &c);
+hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream_t s);
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int pad4(int f) { return (f + 3) & ~3; }
 // width of an internal matrix that an SpMM gathers from: rows start on 128-byte lines and fill whole feature tiles
