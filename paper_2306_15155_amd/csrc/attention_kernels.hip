@@ -7,11 +7,16 @@
 //     dq_i = sum_j ds k_j,  dk_j = sum_i ds q_i,  dv_j = sum_i p keep/(1-p_drop) dy_i,  dbias[h, b] = sum dt,  ds = dt (1 - tanh^2) scale
 // as two walks, one over the rows (dq, dbias) and one over the transposed pattern (dk, dv), so that no sum needs an atomic.
 //
-// What bounds these walks is the gathering of k and v (q and dy) rows from the caches: an entry takes 2 d elements a head for 4 d
-// operations.  A head's vector is spread over G lanes, eight elements (four for heads of at most 16) a lane; a group of lanes takes the same
+// D comes from Y; where Y was rounded to 16 bits, what the rounding took from D is summed along (delta) and taken out of dq at the row's end,
+// and dbias is summed by the walk over the columns, which has the whole D.
+//
+// What bounds these walks is the gathering of k and v (q and dy) rows from the caches, and behind it the instructions around four operations an
+// element.  A head's vector is spread over G lanes, eight elements (four for heads of at most 16) a lane; a group of lanes takes the same
 // entry for a few neighbouring heads (a bundle), so that a gather fills a 128-byte line and shared key heads are read once; and every group
-// walks a chunk of consecutive entries by itself, four at a time.  Rows that cross chunks leave a piece per chunk in scratch, joined by
-// a second kernel in chunk order: results do not depend on scheduling.
+// walks a chunk of consecutive entries by itself, four at a time.  The four dot products are summed so that every lane of a quad ends up
+// with one of them: cap, bias, mask, exponential and generator are worked out once an entry and head (not in every lane), and the
+// weights are handed round by moves within the quad.  Rows that cross chunks leave a piece per chunk in scratch, joined by a second kernel
+// in chunk order: results do not depend on scheduling.
 #include "element_types.h"
 #include "sensei_internal.h"
 
@@ -19,7 +24,8 @@ namespace sensei {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kBatch = 4;
+constexpr int kThreads = 256, kBatch = 4;
+__device__ __forceinline__ int waves() { return (int)(blockDim.x >> 6); }
 
 struct WalkPattern {
     const int32_t *row_ptr, *col;
@@ -42,7 +48,7 @@ struct AttnArgs {
     int bundle_log;               // heads of a bundle: 1 << bundle_log
     DropKey key;                  // threshold 0: nothing is dropped
     float *piece;                 // sums of row pieces: (chunk, first or last piece, head) x G * VEC floats (twice that where two sums are kept)
-    float2 *piece_ml;
+    float2 *piece_ml;             // (m, l) of a row piece; backward over the rows: (delta, -)
     float *bias_part;             // a block's share of dbias, null: not asked for
 };
 
@@ -51,55 +57,178 @@ struct AttnArgs {
 template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)); }
 template <int CTRL> __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
 
-// sum over the G lanes of a head, in all of them (G neighbouring lanes are always active together)
+__device__ __forceinline__ float from_16_away(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
+
+// sum over the four lanes of a quad, in all of them
+__device__ __forceinline__ float quad_sum(float x) {
+    x += dpp<0xB1>(x);          // the neighbour in a pair
+    return x + dpp<0x4E>(x);    // the other pair
+}
+// sum over the G lanes of a head, in all of them (the lanes of a head are always active together)
 template <int G> __device__ __forceinline__ float head_sum(float x) {
-    x += dpp<0xB1>(x);                       // the neighbour in a pair
-    x += dpp<0x4E>(x);                       // the other pair of a quad
+    x = quad_sum(x);
     if (G >= 8) x += dpp<0x141>(x);          // mirrored within eight lanes
     if (G >= 16) x += dpp<0x140>(x);         // mirrored within sixteen
-    if (G >= 32) x += __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F));   // sixteen lanes away
+    if (G >= 32) x += from_16_away(x);
     return x;
 }
+// four sums over the G lanes of a head at once, sum t % 4 in lane t
+template <int G> __device__ __forceinline__ float four_sums(const float (&s)[4], int t) {
+    float a0 = s[0], a1 = s[1], a2 = s[2], a3 = s[3];
+    if (G == 8) {
+        a0 += dpp<0x141>(a0); a1 += dpp<0x141>(a1); a2 += dpp<0x141>(a2); a3 += dpp<0x141>(a3);
+    }
+    const bool odd = t & 1, high = t & 2;
+    float lo = odd ? a1 : a0, hi = odd ? a3 : a2;
+    lo += dpp<0xB1>(odd ? a0 : a1);
+    hi += dpp<0xB1>(odd ? a2 : a3);
+    float x = high ? hi : lo;
+    x += dpp<0x4E>(high ? lo : hi);
+    if (G >= 16) {      // quads of a row of sixteen lanes, turned by one and by two
+        x += dpp<0x124>(x);
+        x += dpp<0x128>(x);
+    }
+    if (G >= 32) x += from_16_away(x);
+    return x;
+}
+// what lane U of the quad holds
+template <int U> __device__ __forceinline__ float of_quad(float x) { return dpp<U * 0x55>(x); }
+template <int U> __device__ __forceinline__ int of_quad(int x) { return dpp<U * 0x55>(x); }
+__device__ __forceinline__ int own_of(int t, int x0, int x1, int x2, int x3) { return t & 2 ? (t & 1 ? x3 : x2) : (t & 1 ? x1 : x0); }
 
-// a lane's share of a head's vector: PIECES pieces of PER elements, piece r at element (r G + t) PER, so that the lanes of a head read side by side
-template <class T, int VEC, int G> struct Share {
+// A lane's share of a head's vector of d elements: PIECES pieces of PER, piece r from element at(r) = (r G + t) PER on, so that the lanes of a head read
+// side by side.  Where the vector ends inside a piece the lane reads the last PER elements instead and leaves those before at(r) to the lane
+// whose they are: every gather is a full piece within its row.  GENERIC (vectors shorter than a piece, matrices past 32-bit offsets): elements one by
+// one where a piece is not whole, 64-bit offsets.
+template <class T, int VEC, int G, bool GENERIC> struct Lanes {
     static constexpr int PER = VEC < kPerPiece<T> ? VEC : kPerPiece<T>, PIECES = VEC / PER;
+    __device__ __forceinline__ static int at(int r, int t) { return (r * G + t) * PER; }
+    __device__ __forceinline__ static int from(int r, int t, int d) { return GENERIC || at(r, t) + PER <= d ? at(r, t) : d - PER; }
+};
+
+// gathered elements as they came: packed pairs in 16 bits
+template <class T, int VEC> struct Gathered {
+    static constexpr int WORDS = VEC * (int)sizeof(T) / 4;
+    unsigned w[WORDS];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) w[k] = 0u;
+    }
+    __device__ __forceinline__ float get(int k) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+        else return to_f32(T{(unsigned short)(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xFFFFu)});
+    }
+};
+template <class T, int VEC> __device__ __forceinline__ float dot(const Gathered<T, VEC> &a, const Gathered<T, VEC> &b) {
+    float s = 0.f;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) s = fmaf(a.get(k), b.get(k), s);
+    } else {
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) {   // products of 16-bit numbers are exact in fp32, sums are held in it
+            if constexpr (__is_same(T, Bf16)) {
+                typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+                s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Pair, a.w[k]), __builtin_bit_cast(Pair, b.w[k]), s, false);
+            } else {
+                typedef _Float16 Pair __attribute__((ext_vector_type(2)));
+                s = __builtin_amdgcn_fdot2(__builtin_bit_cast(Pair, a.w[k]), __builtin_bit_cast(Pair, b.w[k]), s, false);
+            }
+        }
+    }
+    return s;
+}
+
+// where a lane's pieces of a head lie in a matrix: for gathers by row number
+template <class T, int VEC, int G, bool GENERIC> struct Source {
+    using L = Lanes<T, VEC, G, GENERIC>;
+    const char *base;            // the same in every lane
+    unsigned offset[L::PIECES];  // bytes
+    unsigned ld24;
+    long long ld;
+    int t, d;
+    __device__ __forceinline__ Source(const void *p, long long ld_, int first, int d_, int t_) : base(static_cast<const char *>(p)), t(t_), d(d_) {
+        ld = ld_ * (long long)sizeof(T);
+        ld24 = (unsigned)ld;
+#pragma unroll
+        for (int r = 0; r < L::PIECES; ++r) offset[r] = (unsigned)(first + L::from(r, t, d)) * (unsigned)sizeof(T);
+    }
+    // `more`: bytes that are the same in every lane
+    __device__ __forceinline__ Gathered<T, VEC> row(int i, long long more = 0) const {
+        Gathered<T, VEC> x;
+#pragma unroll
+        for (int r = 0; r < L::PIECES; ++r) {
+            if constexpr (!GENERIC) {
+                *reinterpret_cast<Piece<T, L::PER> *>(x.w + r * (L::PER * (int)sizeof(T) / 4)) =
+                    Piece<T, L::PER>::load(reinterpret_cast<const T *>((base + more) + (__umul24((unsigned)i, ld24) + offset[r])));
+            } else {
+                const T *p = reinterpret_cast<const T *>(base + more + (long long)i * ld + offset[r]);
+                const int left = d - L::at(r, t);
+                Piece<T, L::PER> y;
+                if (left >= L::PER) y = Piece<T, L::PER>::load(p);
+                else {
+#pragma unroll
+                    for (int k = 0; k < L::PER; ++k) y.x[k] = k < left ? p[k] : T{};
+                }
+                *reinterpret_cast<Piece<T, L::PER> *>(x.w + r * (L::PER * (int)sizeof(T) / 4)) = y;
+            }
+        }
+        return x;
+    }
+    // the elements that are this lane's own, 0 in the place of the others
+    __device__ __forceinline__ Gathered<T, VEC> own(int i) const {
+        Gathered<T, VEC> x;
+#pragma unroll
+        for (int r = 0; r < L::PIECES; ++r) {
+            const T *p = reinterpret_cast<const T *>(base + (long long)i * ld + offset[r]);
+            const int first = L::at(r, t), from = L::from(r, t, d);
+            Piece<T, L::PER> y;
+#pragma unroll
+            for (int k = 0; k < L::PER; ++k) y.x[k] = T{};
+            if (from == first && first + L::PER <= d) y = Piece<T, L::PER>::load(p);
+            else {
+#pragma unroll
+                for (int k = 0; k < L::PER; ++k)
+                    if (from + k >= first && from + k < d) y.x[k] = p[k];
+            }
+            *reinterpret_cast<Piece<T, L::PER> *>(x.w + r * (L::PER * (int)sizeof(T) / 4)) = y;
+        }
+        return x;
+    }
+};
+
+// sums of a lane's share
+template <class T, int VEC, int G, bool GENERIC> struct Sums {
+    using L = Lanes<T, VEC, G, GENERIC>;
     float v[VEC];
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v[k] = 0.f;
     }
-    __device__ __forceinline__ void load(const T *p, int t, int d) {
+    __device__ __forceinline__ void add(float w, const Gathered<T, VEC> &x) {
 #pragma unroll
-        for (int r = 0; r < PIECES; ++r) {
-            const int at = (r * G + t) * PER;
-            if (at + PER <= d) {
-                const Piece<T, PER> x = Piece<T, PER>::load(p + at);
+        for (int k = 0; k < VEC; ++k) v[k] = fmaf(w, x.get(k), v[k]);
+    }
+    __device__ __forceinline__ void add(float w, const Sums &x) {
 #pragma unroll
-                for (int k = 0; k < PER; ++k) v[r * PER + k] = to_f32(x.x[k]);
-            } else {
+        for (int k = 0; k < VEC; ++k) v[k] = fmaf(w, x.v[k], v[k]);
+    }
+    __device__ __forceinline__ void scale(float w) {
 #pragma unroll
-                for (int k = 0; k < PER; ++k) v[r * PER + k] = 0.f;
-                if (at < d) {
-#pragma unroll
-                    for (int k = 0; k < PER; ++k)
-                        if (at + k < d) v[r * PER + k] = to_f32(p[at + k]);
-                }
-            }
-        }
+        for (int k = 0; k < VEC; ++k) v[k] *= w;
     }
     __device__ __forceinline__ void store(T *p, int t, int d, float by) const {
 #pragma unroll
-        for (int r = 0; r < PIECES; ++r) {
-            const int at = (r * G + t) * PER;
-            Piece<T, PER> x;
+        for (int r = 0; r < L::PIECES; ++r) {
+            const int first = L::at(r, t), from = L::from(r, t, d);
+            Piece<T, L::PER> x;
 #pragma unroll
-            for (int k = 0; k < PER; ++k) x.x[k] = from_f32<T>(v[r * PER + k] * by);
-            if (at + PER <= d) x.store(p + at);
-            else if (at < d) {
+            for (int k = 0; k < L::PER; ++k) x.x[k] = from_f32<T>(v[r * L::PER + k] * by);
+            if (from == first && first + L::PER <= d) x.store(p + first);
+            else {
 #pragma unroll
-                for (int k = 0; k < PER; ++k)
-                    if (at + k < d) p[at + k] = x.x[k];
+                for (int k = 0; k < L::PER; ++k)
+                    if (from + k >= first && from + k < d) p[from + k] = x.x[k];
             }
         }
     }
@@ -114,20 +243,6 @@ template <class T, int VEC, int G> struct Share {
             const float4 x = *reinterpret_cast<const float4 *>(p + t * VEC + k);
             v[k] = x.x; v[k + 1] = x.y; v[k + 2] = x.z; v[k + 3] = x.w;
         }
-    }
-    __device__ __forceinline__ float dot(const Share &o) const {
-        float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) s = fmaf(v[k], o.v[k], s);
-        return s;
-    }
-    __device__ __forceinline__ void add(float w, const Share &o) {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) v[k] = fmaf(w, o.v[k], v[k]);
-    }
-    __device__ __forceinline__ void scale(float w) {
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) v[k] *= w;
     }
 };
 
@@ -167,6 +282,16 @@ struct Walk {
         const int n = (row_end < end ? row_end : end) - e;
         return n < kBatch ? n : kBatch;
     }
+    // columns of the batch: behind its n entries the first one again, which is there to be read
+    __device__ __forceinline__ void columns(int n, int (&c)[kBatch]) const {
+        c[0] = col[0];
+#pragma unroll
+        for (int u = 1; u < kBatch; ++u) c[u] = u < n ? col[u] : col[0];
+    }
+    __device__ __forceinline__ int own_bucket(int t, int n_buckets) const {
+        const int b = (int)(bucket >> (8 * (t & 3)) & 255u);
+        return b < n_buckets ? b : n_buckets - 1;
+    }
     __device__ __forceinline__ bool row_done() const { return e == row_end || e == end; }
     // the row of entry e, which lies behind row i: the next one, or across a run of empty rows by doubling steps and halving
     __device__ __forceinline__ void next_row(const WalkPattern &p) {
@@ -199,7 +324,7 @@ template <int G> struct Place {
         slot = lane / G;
         in_bundle = slot & ((1 << bundle_log) - 1);
         const int head = ((int)blockIdx.y << bundle_log) + in_bundle;
-        chunk = ((int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6)) * groups + (slot >> bundle_log);
+        chunk = ((int)blockIdx.x * waves() + (int)(threadIdx.x >> 6)) * groups + (slot >> bundle_log);
         live = head < n_heads && chunk < n_chunks;
         h = head < n_heads ? head : n_heads - 1;
     }
@@ -219,32 +344,20 @@ __device__ __forceinline__ Tanh tanh_of(float x) {
     return a < 0.25f ? Tanh{s, fmaf(-s, s, 1.f)} : Tanh{copysignf((1.f - y) * r, x), 4.f * y * r * r};
 }
 
-// the bundle's bias table in LDS; every thread of the workgroup comes here
-__device__ __forceinline__ const float *load_bias(const AttnArgs &a, float *lds) {
-    if (!a.bias) return nullptr;
-    const int n = a.n_buckets << a.bundle_log, first = ((int)blockIdx.y << a.bundle_log) * a.n_buckets, all = a.heads * a.n_buckets;
-    for (int k = threadIdx.x; k < n; k += kThreads) lds[k] = first + k < all ? a.bias[first + k] : 0.f;
-    __syncthreads();
-    return lds;
-}
-__device__ __forceinline__ int bucket_of(const AttnArgs &a, unsigned four, int u) {
-    const int b = (int)(four >> (8 * u) & 255u);
-    return b < a.n_buckets ? b : a.n_buckets - 1;
+// a score and what it does to the gradient
+struct Score { float x, slope; };
+__device__ __forceinline__ Score score_of(const AttnArgs &a, float dot) {
+    const float x = dot * a.scale;
+    if (!(a.cap > 0.f)) return {x, 1.f};
+    const Tanh th = tanh_of(x * a.inv_cap);
+    return {a.cap * th.value, th.slope};
 }
 
-// Which of the four entries (row of the pattern: row[u], column: col[u]) keep their weight for query head h.  A quad of lanes works out an entry each
-// and hands the answers round: one generator call a lane and batch.
-__device__ __forceinline__ void keep_flags(const DropKey &key, unsigned offset, const int *row, const int *col, int h, int t, bool *keep) {
-    const int u = t & 3;
-    const unsigned r = (unsigned)(u & 2 ? (u & 1 ? row[3] : row[2]) : (u & 1 ? row[1] : row[0]));
-    const unsigned c = (unsigned)(u & 2 ? (u & 1 ? col[3] : col[2]) : (u & 1 ? col[1] : col[0]));
-    const Words w = philox(c, r, 0x80000000u | (unsigned)(h >> 2), offset, key.k0, key.k1);
-    const unsigned mine = h & 2 ? (h & 1 ? w.w[3] : w.w[2]) : (h & 1 ? w.w[1] : w.w[0]);
-    const int kept = mine >= key.threshold;
-    keep[0] = dpp<0x00>(kept) != 0;
-    keep[1] = dpp<0x55>(kept) != 0;
-    keep[2] = dpp<0xAA>(kept) != 0;
-    keep[3] = dpp<0xFF>(kept) != 0;
+// does the weight of entry (row, col) stay for query head h?
+__device__ __forceinline__ bool kept(const DropKey &key, unsigned offset, int row, int col, int h) {
+    const Words w = philox((unsigned)col, (unsigned)row, 0x80000000u | (unsigned)(h >> 2), offset, key.k0, key.k1);
+    const unsigned w0 = w.w[0], w1 = w.w[1], w2 = w.w[2], w3 = w.w[3];
+    return (h & 2 ? (h & 1 ? w3 : w2) : (h & 1 ? w1 : w0)) >= key.threshold;
 }
 __device__ __forceinline__ unsigned drop_offset(const DropKey &key) { return key.offset + (key.offset_dev ? *key.offset_dev : 0u); }
 
@@ -253,82 +366,73 @@ __device__ __forceinline__ size_t piece_at(int chunk, bool goes_on, int heads, i
 
 // ------------------------------------------------------------------------------------------------------------------ forward
 
-template <class T, int VEC, int G>
+template <class T, int VEC, int G, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
-    extern __shared__ float lds[];
-    const float *bias = load_bias(a, lds);
     const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
     if (!at.live) return;
     const int h = at.h, g = h / a.ratio, t = at.t;
-    const T *Q = static_cast<const T *>(a.Q) + (size_t)h * a.d, *K = static_cast<const T *>(a.K) + (size_t)g * a.d, *V = static_cast<const T *>(a.V) + (size_t)g * a.dv;
+    const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, h * a.d, a.d, t), K(a.K, a.ldk, g * a.d, a.d, t), V(a.V, a.ldv, g * a.dv, a.dv, t);
     T *Y = static_cast<T *>(a.O1) + (size_t)h * a.dv;
-    if (bias) bias += at.in_bundle * a.n_buckets;
+    const float *bias = a.bias ? a.bias + h * a.n_buckets : nullptr;
     const unsigned offset = drop_offset(a.key);
     Walk w;
     w.begin(a.p, at.chunk);
-    Share<T, VEC, G> q, acc;
-    q.load(Q + (long long)w.i * a.ldq, t, a.d);
+    Gathered<T, VEC> q = Q.own(w.i);
+    Sums<T, VEC, G, GENERIC> acc;
     acc.zero();
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f;    // l: the lane's own entries
     while (w.e < w.end) {
         const int n = w.count();
-        int col[kBatch], row[kBatch];
-        bool use[kBatch], keep[kBatch];
-        float x[kBatch], b[kBatch];
+        int col[kBatch];
+        w.columns(n, col);
+        Gathered<T, VEC> k[kBatch], v[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            col[u] = w.col[u];
-            row[u] = w.i;
-            use[u] = u < n;
-            keep[u] = true;
-            b[u] = bias ? bias[bucket_of(a, w.bucket, u)] : 0.f;
-            use[u] = use[u] && b[u] != -INFINITY;    // a masked entry has no share, whatever its key and value hold
+        for (int u = 0; u < kBatch; ++u) k[u] = K.row(col[u]);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
+        bool use = (t & 3) < n, keep = true;
+        float b = 0.f;
+        if (bias) {
+            b = bias[w.own_bucket(t, a.n_buckets)];
+            use = use && b != -INFINITY;
         }
+        if (a.key.threshold) keep = kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-        if (a.key.threshold) keep_flags(a.key, offset, row, col, h, t, keep);
-        Share<T, VEC, G> k[kBatch], v[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            k[u].zero();
-            if (use[u]) k[u].load(K + (long long)col[u] * a.ldk, t, a.d);
+        if (bias && __any((t & 3) < n && !use)) {   // a masked entry has no share, whatever its key and value hold
+            if (!of_quad<0>((int)use)) v[0].zero();
+            if (!of_quad<1>((int)use)) v[1].zero();
+            if (!of_quad<2>((int)use)) v[2].zero();
+            if (!of_quad<3>((int)use)) v[3].zero();
         }
+        float s[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            v[u].zero();
-            if (use[u] && keep[u]) v[u].load(V + (long long)col[u] * a.ldv, t, a.dv);
-        }
-        float top = m;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            x[u] = head_sum<G>(q.dot(k[u])) * a.scale;
-            if (a.cap > 0.f) x[u] = a.cap * tanh_of(x[u] * a.inv_cap).value;
-            x[u] = use[u] ? x[u] + b[u] : -INFINITY;
-            top = fmaxf(top, x[u]);
-        }
-        const float base = top > -INFINITY ? top : 0.f;
-        const float f = exp_neg(m - base);
+        for (int u = 0; u < kBatch; ++u) s[u] = dot(q, k[u]);
+        const Score sc = score_of(a, four_sums<G>(s, t));   // every lane takes part, whatever its entry
+        const float x = use ? sc.x + b : -INFINITY;
+        float top = fmaxf(x, dpp<0xB1>(x));
+        top = fmaxf(m, fmaxf(top, dpp<0x4E>(top)));
+        const float base = top > -INFINITY ? top : 0.f, f = exp_neg(m - base), p = exp_neg(x - base), kp = keep ? p : 0.f;
         m = top;
-        l *= f;
+        l = fmaf(l, f, p);
         acc.scale(f);
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const float p = exp_neg(x[u] - base);
-            l += p;
-            acc.add(keep[u] ? p : 0.f, v[u]);
-        }
+        acc.add(of_quad<0>(kp), v[0]);
+        acc.add(of_quad<1>(kp), v[1]);
+        acc.add(of_quad<2>(kp), v[2]);
+        acc.add(of_quad<3>(kp), v[3]);
         w.e += n;
         if (w.row_done()) {
+            const float sum = quad_sum(l);
             if (!w.goes_on && w.e == w.row_end) {
-                acc.store(Y + (long long)w.i * a.ldo1, t, a.dv, l == 0.f ? 0.f : a.key.keep_scale / l);
-                if (t == 0) a.stats[(size_t)w.i * a.heads + h] = make_float2(m, logf(l));
+                acc.store(Y + (long long)w.i * a.ldo1, t, a.dv, sum == 0.f ? 0.f : a.key.keep_scale / sum);
+                if (t == 0) a.stats[(size_t)w.i * a.heads + h] = make_float2(m, logf(sum));
             } else {
-                const size_t s = piece_at(at.chunk, w.goes_on, a.heads, h);
-                acc.put(a.piece + s * (G * VEC), t);
-                if (t == 0) a.piece_ml[s] = make_float2(m, l);
+                const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
+                acc.put(a.piece + at_piece * (G * VEC), t);
+                if (t == 0) a.piece_ml[at_piece] = make_float2(m, sum);
             }
             if (w.e < w.end) {
                 w.next_row(a.p);
-                q.load(Q + (long long)w.i * a.ldq, t, a.d);
+                q = Q.own(w.i);
                 acc.zero();
                 m = -INFINITY;
                 l = 0.f;
@@ -339,102 +443,218 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
 
 // ------------------------------------------------------------------------------------------------------------------ backward, over the rows
 
-template <class T, int VEC, int G>
+template <class T, int VEC, int G, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
-    extern __shared__ float lds[];
-    const float *bias = load_bias(a, lds);
+    constexpr bool WHOLE_Y = sizeof(T) == 4;     // Y holds what D needs
     const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
-    // dbias: a table of its own for every head of every group, so that its sums have one order
-    float *tables = lds + ((a.n_buckets << a.bundle_log) + 3) / 4 * 4, *mine = tables + ((threadIdx.x >> 6) * (64 / G) + at.slot) * a.n_buckets;
+    if (!at.live) return;
+    const int h = at.h, g = h / a.ratio, t = at.t;
+    const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, h * a.d, a.d, t), K(a.K, a.ldk, g * a.d, a.d, t), V(a.V, a.ldv, g * a.dv, a.dv, t), Y(a.Y, a.ldy, h * a.dv, a.dv, t),
+        dY(a.dY, a.lddy, h * a.dv, a.dv, t);
+    T *dQ = static_cast<T *>(a.O1) + (size_t)h * a.d;
+    const float *bias = a.bias ? a.bias + h * a.n_buckets : nullptr;
+    const unsigned offset = drop_offset(a.key);
+    Walk w;
+    w.begin(a.p, at.chunk);
+    Gathered<T, VEC> q, dy;
+    Sums<T, VEC, G, GENERIC> acc, share;         // sum of ds k; of alpha slope scale k, which delta is taken out by
+    float m, log_l, D, delta;
+    auto enter = [&]() {
+        q = Q.own(w.i);
+        dy = dY.own(w.i);
+        const Gathered<T, VEC> y = Y.own(w.i);
+        const float2 ml = a.stats[(size_t)w.i * a.heads + h];
+        m = ml.x;
+        log_l = ml.y;
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) s = fmaf(dy.get(k), y.get(k), s);
+        D = head_sum<G>(s);
+        if (!w.goes_on && t == 0) a.row_stats[(size_t)w.i * a.heads + h] = make_float4(m, log_l, D, 0.f);
+        acc.zero();
+        if (!WHOLE_Y) share.zero();
+        delta = 0.f;
+    };
+    enter();
+    while (w.e < w.end) {
+        const int n = w.count();
+        int col[kBatch];
+        w.columns(n, col);
+        Gathered<T, VEC> k[kBatch], v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) k[u] = K.row(col[u]);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
+        bool use = (t & 3) < n, keep = true;
+        float b = 0.f;
+        if (bias) {
+            b = bias[w.own_bucket(t, a.n_buckets)];
+            use = use && b != -INFINITY;
+        }
+        if (a.key.threshold) keep = kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h);
+        if (w.e + n < w.end) w.fetch(a.p, w.e + n);
+        if (bias && __any((t & 3) < n && !use)) {
+            if (!of_quad<0>((int)use)) k[0].zero();
+            if (!of_quad<1>((int)use)) k[1].zero();
+            if (!of_quad<2>((int)use)) k[2].zero();
+            if (!of_quad<3>((int)use)) k[3].zero();
+        }
+        float s[kBatch], o[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            s[u] = dot(q, k[u]);
+            o[u] = dot(dy, v[u]);
+        }
+        const Score sc = score_of(a, four_sums<G>(s, t));
+        const float dot_v = four_sums<G>(o, t), dp = keep ? dot_v * a.key.keep_scale : 0.f;
+        const float p = use ? exp_neg((sc.x + b - m) - log_l) : 0.f, dt = use ? p * (dp - D) : 0.f;
+        const float by = sc.slope * a.scale, ds = dt * by;
+        acc.add(of_quad<0>(ds), k[0]);
+        acc.add(of_quad<1>(ds), k[1]);
+        acc.add(of_quad<2>(ds), k[2]);
+        acc.add(of_quad<3>(ds), k[3]);
+        if (!WHOLE_Y) {
+            delta += dt;
+            const float pb = p * by;
+            share.add(of_quad<0>(pb), k[0]);
+            share.add(of_quad<1>(pb), k[1]);
+            share.add(of_quad<2>(pb), k[2]);
+            share.add(of_quad<3>(pb), k[3]);
+        }
+        w.e += n;
+        if (w.row_done()) {
+            const float off = WHOLE_Y ? 0.f : quad_sum(delta);
+            if (!w.goes_on && w.e == w.row_end) {
+                if (!WHOLE_Y) {
+                    acc.add(-off, share);
+                    if (t == 0) a.row_stats[(size_t)w.i * a.heads + h].z = D + off;
+                }
+                acc.store(dQ + (long long)w.i * a.ldo1, t, a.d, 1.f);
+            } else {
+                const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
+                float *to = a.piece + at_piece * ((WHOLE_Y ? 1 : 2) * G * VEC);
+                acc.put(to, t);
+                if (!WHOLE_Y) {
+                    share.put(to + G * VEC, t);
+                    if (t == 0) a.piece_ml[at_piece] = make_float2(off, 0.f);
+                }
+            }
+            if (w.e < w.end) {
+                w.next_row(a.p);
+                enter();
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------ backward, over the columns
+
+// The walk goes over the transposed pattern: its rows are the columns j, its entries the rows i that attend to them.  A lane stays with one key
+// head and takes that head's query heads one after the other.  dbias is summed in LDS, in a table of their own for every head of every
+// group, so that the sums have one order.
+template <class T, int VEC, int G, bool GENERIC>
+__global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
+    extern __shared__ float tables[];
+    const Place<G> at(a.kv_heads, a.p.n_chunks, a.bundle_log);
+    const int per = a.ratio * a.n_buckets;
+    float *table = tables + ((int)(threadIdx.x >> 6) * (64 / G) + at.slot) * per;
     if (a.bias_part) {
-        for (int k = threadIdx.x; k < kWaves * (64 / G) * a.n_buckets; k += kThreads) tables[k] = 0.f;
+        for (int k = threadIdx.x; k < waves() * (64 / G) * per; k += (int)blockDim.x) tables[k] = 0.f;
         __syncthreads();
     }
     if (at.live) {
-        const int h = at.h, g = h / a.ratio, t = at.t;
-        const T *Q = static_cast<const T *>(a.Q) + (size_t)h * a.d, *K = static_cast<const T *>(a.K) + (size_t)g * a.d, *V = static_cast<const T *>(a.V) + (size_t)g * a.dv;
-        const T *Y = static_cast<const T *>(a.Y) + (size_t)h * a.dv, *dY = static_cast<const T *>(a.dY) + (size_t)h * a.dv;
-        T *dQ = static_cast<T *>(a.O1) + (size_t)h * a.d;
-        const float *my_bias = bias ? bias + at.in_bundle * a.n_buckets : nullptr;
+        const int g = at.h, t = at.t;
+        const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, g * a.ratio * a.d, a.d, t), dY(a.dY, a.lddy, g * a.ratio * a.dv, a.dv, t), K(a.K, a.ldk, g * a.d, a.d, t),
+            V(a.V, a.ldv, g * a.dv, a.dv, t);
+        T *dK = static_cast<T *>(a.O1) + (size_t)g * a.d, *dV = static_cast<T *>(a.O2) + (size_t)g * a.dv;
+        const float *bias = a.bias ? a.bias + g * per : nullptr;
         const unsigned offset = drop_offset(a.key);
         Walk w;
         w.begin(a.p, at.chunk);
-        Share<T, VEC, G> q, dy, acc;
-        float m, log_l, D;
-        auto enter = [&]() {
-            Share<T, VEC, G> y;
-            q.load(Q + (long long)w.i * a.ldq, t, a.d);
-            dy.load(dY + (long long)w.i * a.lddy, t, a.dv);
-            y.load(Y + (long long)w.i * a.ldy, t, a.dv);
-            const float2 ml = a.stats[(size_t)w.i * a.heads + h];
-            m = ml.x;
-            log_l = ml.y;
-            D = head_sum<G>(dy.dot(y));
-            if (!w.goes_on && t == 0) a.row_stats[(size_t)w.i * a.heads + h] = make_float4(m, log_l, D, 0.f);
-            acc.zero();
-        };
-        enter();
+        Gathered<T, VEC> k = K.own(w.i), v = V.own(w.i);
+        Sums<T, VEC, G, GENERIC> dk, dv;
+        dk.zero();
+        dv.zero();
         while (w.e < w.end) {
             const int n = w.count();
-            int col[kBatch], row[kBatch], bin[kBatch];
-            bool use[kBatch], keep[kBatch];
-            float b[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                col[u] = w.col[u];
-                row[u] = w.i;
-                keep[u] = true;
-                bin[u] = my_bias ? bucket_of(a, w.bucket, u) : 0;
-                b[u] = my_bias ? my_bias[bin[u]] : 0.f;
-                use[u] = u < n && b[u] != -INFINITY;
-            }
+            int row[kBatch];
+            w.columns(n, row);
+            const int own = own_of(t, row[0], row[1], row[2], row[3]), bin = bias ? w.own_bucket(t, a.n_buckets) : 0;
             if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-            if (a.key.threshold) keep_flags(a.key, offset, row, col, h, t, keep);
-            Share<T, VEC, G> k[kBatch], v[kBatch];
+            for (int r = 0; r < a.ratio; ++r) {
+                const int h = g * a.ratio + r;
+                Gathered<T, VEC> q[kBatch], dy[kBatch];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                k[u].zero();
-                if (use[u]) k[u].load(K + (long long)col[u] * a.ldk, t, a.d);
-            }
+                for (int u = 0; u < kBatch; ++u) q[u] = Q.row(row[u], (long long)r * a.d * (int)sizeof(T));
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                v[u].zero();
-                if (use[u] && keep[u]) v[u].load(V + (long long)col[u] * a.ldv, t, a.dv);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                float x = head_sum<G>(q.dot(k[u])) * a.scale, slope = 1.f;
-                if (a.cap > 0.f) {
-                    const Tanh th = tanh_of(x * a.inv_cap);
-                    x = a.cap * th.value;
-                    slope = th.slope;
+                for (int u = 0; u < kBatch; ++u) dy[u] = dY.row(row[u], (long long)r * a.dv * (int)sizeof(T));
+                const float4 st = a.row_stats[(size_t)own * a.heads + h];
+                bool use = (t & 3) < n, keep = true;
+                float b = 0.f;
+                if (bias) {
+                    b = bias[r * a.n_buckets + bin];
+                    use = use && b != -INFINITY;
                 }
-                const float p = use[u] ? exp_neg((x + b[u] - m) - log_l) : 0.f;
-                const float dp = head_sum<G>(dy.dot(v[u])) * a.key.keep_scale;
-                const float dt = use[u] ? p * (dp - D) : 0.f;
-                if (a.bias_part && t == 0 && use[u]) __hip_atomic_fetch_add(mine + bin[u], dt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                acc.add(dt * slope * a.scale, k[u]);
+                if (a.key.threshold) keep = kept(a.key, offset, own, w.i, h);
+                if (bias && __any((t & 3) < n && !use)) {
+                    if (!of_quad<0>((int)use)) { q[0].zero(); dy[0].zero(); }
+                    if (!of_quad<1>((int)use)) { q[1].zero(); dy[1].zero(); }
+                    if (!of_quad<2>((int)use)) { q[2].zero(); dy[2].zero(); }
+                    if (!of_quad<3>((int)use)) { q[3].zero(); dy[3].zero(); }
+                }
+                float s[kBatch], o[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    s[u] = dot(k, q[u]);
+                    o[u] = dot(v, dy[u]);
+                }
+                const Score sc = score_of(a, four_sums<G>(s, t));
+                const float dot_v = four_sums<G>(o, t), dp = keep ? dot_v * a.key.keep_scale : 0.f;
+                const float p = use ? exp_neg((sc.x + b - st.x) - st.y) : 0.f, dt = use ? p * (dp - st.z) : 0.f;
+                const float ds = dt * sc.slope * a.scale, pw = keep ? p * a.key.keep_scale : 0.f;
+                if (a.bias_part) {   // one lane after the other: two of a quad may be in one bucket
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        if (t == u && use) __hip_atomic_fetch_add(table + r * a.n_buckets + bin, dt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                }
+                dk.add(of_quad<0>(ds), q[0]);
+                dk.add(of_quad<1>(ds), q[1]);
+                dk.add(of_quad<2>(ds), q[2]);
+                dk.add(of_quad<3>(ds), q[3]);
+                dv.add(of_quad<0>(pw), dy[0]);
+                dv.add(of_quad<1>(pw), dy[1]);
+                dv.add(of_quad<2>(pw), dy[2]);
+                dv.add(of_quad<3>(pw), dy[3]);
             }
             w.e += n;
             if (w.row_done()) {
-                if (!w.goes_on && w.e == w.row_end) acc.store(dQ + (long long)w.i * a.ldo1, t, a.d, 1.f);
-                else acc.put(a.piece + piece_at(at.chunk, w.goes_on, a.heads, h) * (G * VEC), t);
+                if (!w.goes_on && w.e == w.row_end) {
+                    dk.store(dK + (long long)w.i * a.ldo1, t, a.d, 1.f);
+                    dv.store(dV + (long long)w.i * a.ldo2, t, a.dv, 1.f);
+                } else {
+                    float *to = a.piece + piece_at(at.chunk, w.goes_on, a.kv_heads, g) * (2 * G * VEC);
+                    dk.put(to, t);
+                    dv.put(to + G * VEC, t);
+                }
                 if (w.e < w.end) {
                     w.next_row(a.p);
-                    enter();
+                    k = K.own(w.i);
+                    v = V.own(w.i);
+                    dk.zero();
+                    dv.zero();
                 }
             }
         }
     }
     if (a.bias_part) {
         __syncthreads();
-        const int n = a.n_buckets << a.bundle_log, per_wave = 64 / G;
-        for (int k = threadIdx.x; k < n; k += kThreads) {
-            const int in_bundle = k / a.n_buckets, b = k % a.n_buckets, h = ((int)blockIdx.y << a.bundle_log) + in_bundle;
-            if (h >= a.heads) continue;
+        const int n = per << a.bundle_log, slots = waves() * (64 / G);
+        for (int k = threadIdx.x; k < n; k += (int)blockDim.x) {
+            const int in_bundle = k / per, g = ((int)blockIdx.y << a.bundle_log) + in_bundle;
+            if (g >= a.kv_heads) continue;
             float s = 0.f;
-            for (int o = in_bundle; o < kWaves * per_wave; o += 1 << a.bundle_log) s += tables[o * a.n_buckets + b];
-            a.bias_part[((size_t)blockIdx.x * a.heads + h) * a.n_buckets + b] = s;
+            for (int o = in_bundle; o < slots; o += 1 << a.bundle_log) s += tables[o * per + k % per];
+            a.bias_part[(size_t)blockIdx.x * a.heads * a.n_buckets + (size_t)g * per + k % per] = s;
         }
     }
 }
@@ -454,119 +674,21 @@ __global__ __launch_bounds__(1024) void k_attention_bias(const float *__restrict
     if (seg == 0 && k < n) out[k] = (float)lds[0][threadIdx.x & 15];
 }
 
-// ------------------------------------------------------------------------------------------------------------------ backward, over the columns
-
-// The walk goes over the transposed pattern: its rows are the columns j, its entries the rows i that attend to them.  A lane stays with one key
-// head and takes that head's query heads one after the other.
-template <class T, int VEC, int G>
-__global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
-    extern __shared__ float lds[];
-    const float *bias = nullptr;
-    const Place<G> at(a.kv_heads, a.p.n_chunks, a.bundle_log);
-    if (a.bias) {   // of all query heads of the bundle's key heads
-        const int per = a.ratio * a.n_buckets, n = per << a.bundle_log, first = ((int)blockIdx.y << a.bundle_log) * per, all = a.heads * a.n_buckets;
-        for (int k = threadIdx.x; k < n; k += kThreads) lds[k] = first + k < all ? a.bias[first + k] : 0.f;
-        __syncthreads();
-        bias = lds + at.in_bundle * per;
-    }
-    if (!at.live) return;
-    const int g = at.h, t = at.t;
-    const T *Q = static_cast<const T *>(a.Q), *dY = static_cast<const T *>(a.dY);
-    const T *K = static_cast<const T *>(a.K) + (size_t)g * a.d, *V = static_cast<const T *>(a.V) + (size_t)g * a.dv;
-    T *dK = static_cast<T *>(a.O1) + (size_t)g * a.d, *dV = static_cast<T *>(a.O2) + (size_t)g * a.dv;
-    const unsigned offset = drop_offset(a.key);
-    Walk w;
-    w.begin(a.p, at.chunk);
-    Share<T, VEC, G> k, v, dk, dv;
-    k.load(K + (long long)w.i * a.ldk, t, a.d);
-    v.load(V + (long long)w.i * a.ldv, t, a.dv);
-    dk.zero();
-    dv.zero();
-    while (w.e < w.end) {
-        const int n = w.count();
-        int col[kBatch], row[kBatch], bin[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            row[u] = w.col[u];
-            col[u] = w.i;
-            bin[u] = bias ? bucket_of(a, w.bucket, u) : 0;
-        }
-        if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-        for (int r = 0; r < a.ratio; ++r) {
-            const int h = g * a.ratio + r;
-            bool use[kBatch], keep[kBatch];
-            float b[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                keep[u] = true;
-                b[u] = bias ? bias[r * a.n_buckets + bin[u]] : 0.f;
-                use[u] = u < n && b[u] != -INFINITY;
-            }
-            if (a.key.threshold) keep_flags(a.key, offset, row, col, h, t, keep);
-            Share<T, VEC, G> q[kBatch], dy[kBatch];
-            float4 st[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                q[u].zero();
-                dy[u].zero();
-                st[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (use[u]) {
-                    q[u].load(Q + (long long)row[u] * a.ldq + (size_t)h * a.d, t, a.d);
-                    st[u] = a.row_stats[(size_t)row[u] * a.heads + h];
-                    if (keep[u]) dy[u].load(dY + (long long)row[u] * a.lddy + (size_t)h * a.dv, t, a.dv);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                float x = head_sum<G>(k.dot(q[u])) * a.scale, slope = 1.f;
-                if (a.cap > 0.f) {
-                    const Tanh th = tanh_of(x * a.inv_cap);
-                    x = a.cap * th.value;
-                    slope = th.slope;
-                }
-                const float p = use[u] ? exp_neg((x + b[u] - st[u].x) - st[u].y) : 0.f;
-                const float dp = head_sum<G>(v.dot(dy[u])) * a.key.keep_scale;
-                const float dt = use[u] ? p * (dp - st[u].z) : 0.f;
-                dk.add(dt * slope * a.scale, q[u]);
-                dv.add(keep[u] ? p * a.key.keep_scale : 0.f, dy[u]);
-            }
-        }
-        w.e += n;
-        if (w.row_done()) {
-            if (!w.goes_on && w.e == w.row_end) {
-                dk.store(dK + (long long)w.i * a.ldo1, t, a.d, 1.f);
-                dv.store(dV + (long long)w.i * a.ldo2, t, a.dv, 1.f);
-            } else {
-                float *s = a.piece + piece_at(at.chunk, w.goes_on, a.kv_heads, g) * (2 * G * VEC);
-                dk.put(s, t);
-                dv.put(s + G * VEC, t);
-            }
-            if (w.e < w.end) {
-                w.next_row(a.p);
-                k.load(K + (long long)w.i * a.ldk, t, a.d);
-                v.load(V + (long long)w.i * a.ldv, t, a.dv);
-                dk.zero();
-                dv.zero();
-            }
-        }
-    }
-}
-
 // ------------------------------------------------------------------------------------------------------------------ rows in pieces, empty rows
 
-enum { kJoinForward = 0, kJoinOne = 1, kJoinTwo = 2 };
+enum { kJoinForward = 0, kJoinRows = 1, kJoinCols = 2 };
 
 // A wavefront per chunk boundary (and bundle of heads): where a row crosses it that crossed none before, the wavefront joins that row's pieces, its
 // groups taking them in turn.  Workgroups behind those (of the first bundle) look over 64 rows a wavefront and write the rows without entries.
-template <class T, int VEC, int G, int MODE>
+template <class T, int VEC, int G, int MODE, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_heads, int join_blocks) {
-    const int lane = threadIdx.x & 63, wave = (int)blockIdx.x * kWaves + (int)(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = (int)blockIdx.x * waves() + (int)(threadIdx.x >> 6);
     if ((int)blockIdx.x >= join_blocks) {
         if (blockIdx.y > 0) return;
-        const long long r0 = ((long long)((int)blockIdx.x - join_blocks) * kWaves + (threadIdx.x >> 6)) * 64;
+        const long long r0 = ((long long)((int)blockIdx.x - join_blocks) * waves() + (threadIdx.x >> 6)) * 64;
         const bool none = r0 + lane < a.p.n_rows && a.p.row_ptr[r0 + lane] == a.p.row_ptr[r0 + lane + 1];
         unsigned long long todo = __ballot(none);
-        const int w1 = MODE == kJoinForward ? n_heads * a.dv : n_heads * a.d, w2 = MODE == kJoinTwo ? n_heads * a.dv : 0;
+        const int w1 = MODE == kJoinForward ? n_heads * a.dv : n_heads * a.d, w2 = MODE == kJoinCols ? n_heads * a.dv : 0;
         while (todo) {
             const long long row = r0 + __builtin_ctzll(todo);
             todo &= todo - 1;
@@ -584,12 +706,14 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
     const int pieces = (a.p.row_ptr[i + 1] - 1) / T0 - (c - 1) + 1;
     const int groups = (64 / G) >> a.bundle_log, t = lane % G, slot = lane / G, group = slot >> a.bundle_log;
     const int head = ((int)blockIdx.y << a.bundle_log) + (slot & ((1 << a.bundle_log) - 1)), h = head < n_heads ? head : n_heads - 1;
-    constexpr int W = MODE == kJoinTwo ? 2 * G * VEC : G * VEC;
-    Share<T, VEC, G> s1, s2;
+    constexpr bool TWO = MODE == kJoinCols || (MODE == kJoinRows && sizeof(T) == 2);
+    constexpr int W = (TWO ? 2 : 1) * G * VEC;
+    using S = Sums<T, VEC, G, GENERIC>;
+    S s1, s2;
     s1.zero();
     s2.zero();
-    float m = -INFINITY, l = 0.f;
-    auto join = [&](float om, float ol, const Share<T, VEC, G> &o) {
+    float m = -INFINITY, l = 0.f, delta = 0.f;
+    auto join = [&](float om, float ol, const S &o) {
         const float top = fmaxf(m, om), base = top > -INFINITY ? top : 0.f, f = exp_neg(m - base), fo = exp_neg(om - base);
         m = top;
         l = l * f + ol * fo;
@@ -598,41 +722,47 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
     };
     for (int k = group; k < pieces; k += groups) {
         const size_t at = piece_at(c - 1 + k, k > 0, n_heads, h);
-        Share<T, VEC, G> x;
+        S x;
         x.get(a.piece + at * W, t);
         if (MODE == kJoinForward) {
             const float2 ml = a.piece_ml[at];
             join(ml.x, ml.y, x);
         } else {
             s1.add(1.f, x);
-            if (MODE == kJoinTwo) {
+            if (TWO) {
                 x.get(a.piece + at * W + G * VEC, t);
                 s2.add(1.f, x);
             }
+            if (MODE == kJoinRows && TWO) delta += a.piece_ml[at].x;
         }
     }
     for (int dist = G << a.bundle_log; dist < 64; dist <<= 1) {
-        Share<T, VEC, G> x;
+        S x;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) x.v[k] = __shfl_xor(s1.v[k], dist, 64);
         if (MODE == kJoinForward) join(__shfl_xor(m, dist, 64), __shfl_xor(l, dist, 64), x);
         else {
             s1.add(1.f, x);
-            if (MODE == kJoinTwo) {
+            if (TWO) {
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) x.v[k] = __shfl_xor(s2.v[k], dist, 64);
                 s2.add(1.f, x);
             }
+            if (MODE == kJoinRows && TWO) delta += __shfl_xor(delta, dist, 64);
         }
     }
     if (group != 0 || head >= n_heads) return;
     if (MODE == kJoinForward) {
         s1.store(static_cast<T *>(a.O1) + (long long)i * a.ldo1 + (size_t)h * a.dv, t, a.dv, l == 0.f ? 0.f : a.key.keep_scale / l);
         if (t == 0) a.stats[(size_t)i * n_heads + h] = make_float2(m, logf(l));
-    } else {
-        s1.store(static_cast<T *>(a.O1) + (long long)i * a.ldo1 + (size_t)h * a.d, t, a.d, 1.f);
-        if (MODE == kJoinTwo) s2.store(static_cast<T *>(a.O2) + (long long)i * a.ldo2 + (size_t)h * a.dv, t, a.dv, 1.f);
+        return;
     }
+    if (MODE == kJoinRows && TWO) {
+        s1.add(-delta, s2);
+        if (t == 0) a.row_stats[(size_t)i * n_heads + h].z += delta;
+    }
+    s1.store(static_cast<T *>(a.O1) + (long long)i * a.ldo1 + (size_t)h * a.d, t, a.d, 1.f);
+    if (MODE == kJoinCols) s2.store(static_cast<T *>(a.O2) + (long long)i * a.ldo2 + (size_t)h * a.dv, t, a.dv, 1.f);
 }
 
 // ------------------------------------------------------------------------------------------------------------------ preparation
@@ -680,13 +810,13 @@ int bundle_log_of(const Shape &s, int n_heads, int together, int bytes) {
 }
 int chunk_of(int64_t nnz, int bundles, int groups) {
     int t = 256;
-    while (t > 16 && nnz / t * bundles / groups < 16384) t >>= 1;
+    while (t > 16 && nnz / t * bundles / groups < 8192) t >>= 1;
     return t;
 }
 
 struct Layout {
     Shape shape;
-    int bundle_log, bundles, groups, chunk, n_chunks, blocks;
+    int bundle_log, bundles, groups, chunk, n_chunks;
     Layout(int64_t nnz, int n_heads, int together, int d, int dv, int elem) {
         shape = shape_of(d, dv);
         bundle_log = bundle_log_of(shape, n_heads, together, (d > dv ? d : dv) * elem);
@@ -694,26 +824,46 @@ struct Layout {
         groups = (64 / shape.lanes) >> bundle_log;
         chunk = chunk_of(nnz, bundles, groups);
         n_chunks = (int)((nnz + chunk - 1) / chunk);
-        blocks = (n_chunks + kWaves * groups - 1) / (kWaves * groups);
     }
+    int blocks(int waves) const { return (n_chunks + waves * groups - 1) / (waves * groups); }
     size_t rows_bytes() const { return align_up((size_t)n_chunks * sizeof(int32_t), 256); }
     size_t piece_bytes(int n_heads, int sums) const { return align_up((size_t)n_chunks * 2 * n_heads * shape.vec * shape.lanes * sums * sizeof(float), 256); }
     size_t ml_bytes(int n_heads) const { return align_up((size_t)n_chunks * 2 * n_heads * sizeof(float2), 256); }
 };
 
+// Wavefronts of a workgroup of the walk over the columns: as many as the tables of dbias leave room for in 64 KB of LDS
+int table_waves(const AttentionCall &c, const Shape &s) {
+    const size_t wave = (size_t)(64 / s.lanes) * (c.heads / c.kv_heads) * c.n_buckets * sizeof(float);
+    return !c.dbias || 4 * wave <= 65536 ? 4 : 2 * wave <= 65536 ? 2 : 1;
+}
+
 struct Room {   // what the backward carves its scratch into
     Layout rows, cols;
-    size_t bucket, stats, piece, bias;
+    int col_waves;
+    size_t bucket, stats, piece, ml, bias;
     Room(const AttentionCall &c)
         : rows(c.A->nnz, c.heads, c.heads / c.kv_heads, c.d, c.dv, c.elem), cols(c.A->nnz, c.kv_heads, 1, c.d, c.dv, c.elem) {
+        col_waves = table_waves(c, cols.shape);
         bucket = c.n_buckets > 0 ? align_up((size_t)c.A->nnz, 256) : 0;
         stats = align_up((size_t)c.A->n_rows * c.heads * sizeof(float4), 256);
-        const size_t p1 = rows.piece_bytes(c.heads, 1), p2 = cols.piece_bytes(c.kv_heads, 2);   // one after the other
+        const size_t p1 = rows.piece_bytes(c.heads, c.elem == 4 ? 1 : 2), p2 = cols.piece_bytes(c.kv_heads, 2);   // one after the other
         piece = p1 > p2 ? p1 : p2;
-        bias = c.n_buckets > 0 && c.dbias ? align_up((size_t)rows.blocks * c.heads * c.n_buckets * sizeof(float), 256) : 0;
+        ml = c.elem == 4 ? 0 : rows.ml_bytes(c.heads);
+        bias = c.n_buckets > 0 && c.dbias ? align_up((size_t)cols.blocks(col_waves) * c.heads * c.n_buckets * sizeof(float), 256) : 0;
     }
-    size_t bytes() const { return rows.rows_bytes() + cols.rows_bytes() + bucket + stats + piece + bias; }
+    size_t bytes() const { return rows.rows_bytes() + cols.rows_bytes() + bucket + stats + piece + ml + bias; }
 };
+
+// Gathers by 24-bit products and 32-bit offsets, whole pieces: every number of a row and of bytes a row below 2^24, every matrix below 4 GB, heads
+// no narrower than a piece.
+bool plain_gathers(const AttentionCall &c, const Shape &s) {
+    const int per = s.vec < 16 / c.elem ? s.vec : 16 / c.elem;
+    if (c.d < per || c.dv < per || c.A->n_rows >= 1 << 24 || c.A->n_cols >= 1 << 24) return false;
+    struct { int64_t rows, ld; } m[] = {{c.A->n_cols, c.ldk}, {c.A->n_cols, c.ldv}, {c.At ? c.A->n_rows : 0, c.ldq}, {c.At ? c.A->n_rows : 0, c.lddy}};
+    for (const auto &x : m)
+        if (x.rows && (x.ld * c.elem >= 1 << 24 || x.rows * x.ld * c.elem > 0xFFFFFFFFll)) return false;
+    return true;
+}
 
 AttnArgs args_of(const AttentionCall &c) {
     AttnArgs a = {};
@@ -732,52 +882,47 @@ WalkPattern pattern_of(const sensei_csr &A, const Layout &l, const uint8_t *buck
     return {A.row_ptr, A.col_idx, bucket, chunk_row, A.n_rows, (int)A.nnz, l.chunk, l.n_chunks};
 }
 
-template <class T, int VEC, int G, int MODE> hipError_t join_and_fill(const AttnArgs &a, const Layout &l, int n_heads, hipStream_t s) {
-    const int join_blocks = l.n_chunks > 1 ? (l.n_chunks - 1 + kWaves - 1) / kWaves : 0, fill = (int)((a.p.n_rows + 64ll * kWaves - 1) / (64 * kWaves));
+template <class T, int VEC, int G, bool GENERIC, int MODE> hipError_t join_and_fill(const AttnArgs &a, const Layout &l, int n_heads, hipStream_t s) {
+    constexpr int waves = kThreads / 64;
+    const int join_blocks = l.n_chunks > 1 ? (l.n_chunks - 1 + waves - 1) / waves : 0, fill = (int)((a.p.n_rows + 64ll * waves - 1) / (64 * waves));
     if (join_blocks + fill == 0) return hipSuccess;
-    hipLaunchKernelGGL((k_attention_join<T, VEC, G, MODE>), dim3(join_blocks + fill, l.bundles), dim3(kThreads), 0, s, a, n_heads, join_blocks);
+    hipLaunchKernelGGL((k_attention_join<T, VEC, G, MODE, GENERIC>), dim3(join_blocks + fill, l.bundles), dim3(kThreads), 0, s, a, n_heads, join_blocks);
     return hipGetLastError();
 }
 
-template <class T, int VEC, int G> hipError_t forward_shape(AttnArgs a, const Layout &l, hipStream_t s) {
-    if (a.p.nnz > 0) {
-        const size_t lds = a.bias ? (size_t)(a.n_buckets << l.bundle_log) * sizeof(float) : 0;
-        hipLaunchKernelGGL((k_attention<T, VEC, G>), dim3(l.blocks, l.bundles), dim3(kThreads), lds, s, a);
-    }
-    return join_and_fill<T, VEC, G, kJoinForward>(a, l, a.heads, s);
+template <class T, int VEC, int G, bool GENERIC> hipError_t forward_shape(AttnArgs a, const Layout &l, hipStream_t s) {
+    if (a.p.nnz > 0) hipLaunchKernelGGL((k_attention<T, VEC, G, GENERIC>), dim3(l.blocks(kThreads / 64), l.bundles), dim3(kThreads), 0, s, a);
+    return join_and_fill<T, VEC, G, GENERIC, kJoinForward>(a, l, a.heads, s);
 }
 
-template <class T, int VEC, int G> hipError_t backward_shape(const AttentionCall &c, AttnArgs a, const Room &room, const WalkPattern &pr, const WalkPattern &pc, hipStream_t s) {
+template <class T, int VEC, int G, bool GENERIC> hipError_t backward_shape(const AttentionCall &c, AttnArgs a, const Room &room, const WalkPattern &pr, const WalkPattern &pc,
+                                                                           hipStream_t s) {
     hipError_t e;
     a.p = pr;
     a.O1 = c.dQ; a.ldo1 = c.lddq;
     a.bundle_log = room.rows.bundle_log;
-    if (pr.nnz > 0) {
-        const size_t table = (size_t)(((a.n_buckets << a.bundle_log) + 3) / 4 * 4);
-        const size_t lds = a.bias ? (table + (a.bias_part ? (size_t)kWaves * (64 / G) * a.n_buckets : 0)) * sizeof(float) : 0;
-        hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G>), dim3(room.rows.blocks, room.rows.bundles), dim3(kThreads), lds, s, a);
-        if (a.bias_part) {
-            const int n = a.heads * a.n_buckets;
-            hipLaunchKernelGGL(k_attention_bias, dim3((n + 15) / 16), dim3(1024), 0, s, a.bias_part, room.rows.blocks, n, c.dbias);
-        }
-    }
-    if ((e = join_and_fill<T, VEC, G, kJoinOne>(a, room.rows, a.heads, s)) != hipSuccess) return e;
+    if (pr.nnz > 0) hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G, GENERIC>), dim3(room.rows.blocks(kThreads / 64), room.rows.bundles), dim3(kThreads), 0, s, a);
+    if ((e = join_and_fill<T, VEC, G, GENERIC, kJoinRows>(a, room.rows, a.heads, s)) != hipSuccess) return e;
     a.p = pc;
     a.O1 = c.dK; a.ldo1 = c.lddk;
     a.O2 = c.dV; a.ldo2 = c.lddv;
     a.bundle_log = room.cols.bundle_log;
     if (pc.nnz > 0) {
-        const size_t lds = a.bias ? (size_t)(a.n_buckets * a.ratio << a.bundle_log) * sizeof(float) : 0;
-        hipLaunchKernelGGL((k_attention_back_cols<T, VEC, G>), dim3(room.cols.blocks, room.cols.bundles), dim3(kThreads), lds, s, a);
+        const int blocks = room.cols.blocks(room.col_waves), n = a.heads * a.n_buckets;
+        const size_t lds = a.bias_part ? (size_t)room.col_waves * (64 / G) * a.ratio * a.n_buckets * sizeof(float) : 0;
+        hipLaunchKernelGGL((k_attention_back_cols<T, VEC, G, GENERIC>), dim3(blocks, room.cols.bundles), dim3(64 * room.col_waves), lds, s, a);
+        if (a.bias_part) hipLaunchKernelGGL(k_attention_bias, dim3((n + 15) / 16), dim3(1024), 0, s, a.bias_part, blocks, n, c.dbias);
     }
-    return join_and_fill<T, VEC, G, kJoinTwo>(a, room.cols, a.kv_heads, s);
+    return join_and_fill<T, VEC, G, GENERIC, kJoinCols>(a, room.cols, a.kv_heads, s);
 }
 
-#define SENSEI_BY_SHAPE(T, shape, CALL)                                                              \
-    (shape.vec == 4 ? CALL(T, 4, 4) : shape.lanes == 4 ? CALL(T, 8, 4) : shape.lanes == 8 ? CALL(T, 8, 8) \
-     : shape.lanes == 16 ? CALL(T, 8, 16) : CALL(T, 8, 32))
-#define SENSEI_BY_TYPE(type, shape, CALL) \
-    (type == SENSEI_F32 ? SENSEI_BY_SHAPE(float, shape, CALL) : type == SENSEI_BF16 ? SENSEI_BY_SHAPE(Bf16, shape, CALL) : SENSEI_BY_SHAPE(F16, shape, CALL))
+#define SENSEI_BY_SHAPE(T, shape, GEN, CALL)                                                                        \
+    (shape.vec == 4 ? CALL(T, 4, 4, GEN) : shape.lanes == 4 ? CALL(T, 8, 4, GEN) : shape.lanes == 8 ? CALL(T, 8, 8, GEN) \
+     : shape.lanes == 16 ? CALL(T, 8, 16, GEN) : CALL(T, 8, 32, GEN))
+#define SENSEI_BY_GATHER(T, shape, plain, CALL) (plain ? SENSEI_BY_SHAPE(T, shape, false, CALL) : SENSEI_BY_SHAPE(T, shape, true, CALL))
+#define SENSEI_BY_TYPE(type, shape, plain, CALL)                                                                  \
+    (type == SENSEI_F32 ? SENSEI_BY_GATHER(float, shape, plain, CALL) : type == SENSEI_BF16 ? SENSEI_BY_GATHER(Bf16, shape, plain, CALL) \
+     : SENSEI_BY_GATHER(F16, shape, plain, CALL))
 
 }  // namespace
 
@@ -803,8 +948,9 @@ hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s) {
         p.scatter0 = (l.n_chunks + kThreads - 1) / kThreads;
         hipLaunchKernelGGL(k_attention_prep, dim3(p.scatter0), dim3(kThreads), 0, s, p);
     }
-#define SENSEI_CALL(T, V, G) forward_shape<T, V, G>(a, l, s)
-    return SENSEI_BY_TYPE(c.type, l.shape, SENSEI_CALL);
+    const bool plain = plain_gathers(c, l.shape);
+#define SENSEI_CALL(T, V, G, GEN) forward_shape<T, V, G, GEN>(a, l, s)
+    return SENSEI_BY_TYPE(c.type, l.shape, plain, SENSEI_CALL);
 #undef SENSEI_CALL
 }
 
@@ -819,6 +965,7 @@ hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream
     uint8_t *bucket_t = reinterpret_cast<uint8_t *>(take(room.bucket));
     a.row_stats = reinterpret_cast<float4 *>(take(room.stats));
     a.piece = reinterpret_cast<float *>(take(room.piece));
+    a.piece_ml = reinterpret_cast<float2 *>(take(room.ml));
     a.bias_part = a.bias && c.dbias ? reinterpret_cast<float *>(take(room.bias)) : nullptr;
     const WalkPattern pr = pattern_of(*c.A, room.rows, a.bias ? c.bucket : nullptr, rows_r), pc = pattern_of(*c.At, room.cols, a.bias ? bucket_t : nullptr, rows_c);
     if (c.A->nnz > 0) {
@@ -833,8 +980,9 @@ hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream
         const hipError_t e = launch_zero_matrix(c.dbias, 1, c.heads * c.n_buckets, c.heads * c.n_buckets, false, s);
         if (e != hipSuccess) return e;
     }
-#define SENSEI_CALL(T, V, G) backward_shape<T, V, G>(c, a, room, pr, pc, s)
-    return SENSEI_BY_TYPE(c.type, room.rows.shape, SENSEI_CALL);
+    const bool plain = plain_gathers(c, room.rows.shape);
+#define SENSEI_CALL(T, V, G, GEN) backward_shape<T, V, G, GEN>(c, a, room, pr, pc, s)
+    return SENSEI_BY_TYPE(c.type, room.rows.shape, plain, SENSEI_CALL);
 #undef SENSEI_CALL
 }
 
