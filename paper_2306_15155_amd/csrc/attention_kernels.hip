@@ -12,7 +12,7 @@
 //
 // What bounds these walks is the gathering of k and v (q and dy) rows from the caches, and behind it the instructions around four operations an
 // element.  A head's vector is spread over G lanes, eight elements (four for heads of at most 16) a lane; a group of lanes takes the same
-// entry for a few neighbouring heads (a bundle), so that a gather fills a 128-byte line and shared key heads are read once; and every group
+// entry for a few neighbouring heads (a bundle), so that a gather takes whole 128-byte lines and shared key heads are read once; and every group
 // walks a chunk of consecutive entries by itself, four at a time.  The four dot products are summed so that every lane of a quad ends up
 // with one of them: cap, bias, mask, exponential and generator are worked out once an entry and head (not in every lane), and the
 // weights are handed round by moves within the quad.  Rows that cross chunks leave a piece per chunk in scratch, joined by a second kernel
@@ -30,7 +30,7 @@ __device__ __forceinline__ int waves() { return (int)(blockDim.x >> 6); }
 struct WalkPattern {
     const int32_t *row_ptr, *col;
     const uint8_t *bucket;        // in this pattern's order, null: none
-    const int32_t *chunk_row;     // row of the first entry of every chunk
+    int32_t *chunk_row;           // row of the first entry of every chunk, written by the walk
     int n_rows, nnz, chunk, n_chunks;
 };
 
@@ -175,24 +175,23 @@ template <class T, int VEC, int G, bool GENERIC> struct Source {
         }
         return x;
     }
-    // the elements that are this lane's own, 0 in the place of the others
-    __device__ __forceinline__ Gathered<T, VEC> own(int i) const {
-        Gathered<T, VEC> x;
+    // 0 in the place of elements that are not this lane's own
+    __device__ __forceinline__ void keep_own(Gathered<T, VEC> &x) const {
 #pragma unroll
         for (int r = 0; r < L::PIECES; ++r) {
-            const T *p = reinterpret_cast<const T *>(base + (long long)i * ld + offset[r]);
-            const int first = L::at(r, t), from = L::from(r, t, d);
-            Piece<T, L::PER> y;
+            const int skip = L::at(r, t) - L::from(r, t, d);   // of the piece's elements; a lane behind the end has none
 #pragma unroll
-            for (int k = 0; k < L::PER; ++k) y.x[k] = T{};
-            if (from == first && first + L::PER <= d) y = Piece<T, L::PER>::load(p);
-            else {
-#pragma unroll
-                for (int k = 0; k < L::PER; ++k)
-                    if (from + k >= first && from + k < d) y.x[k] = p[k];
+            for (int k = 0; k < L::PER; ++k) {
+                unsigned &w = x.w[(r * L::PER + k) * (int)sizeof(T) / 4];
+                if (k < skip) w &= sizeof(T) == 4 ? 0u : k & 1 ? 0xFFFFu : 0xFFFF0000u;
             }
-            *reinterpret_cast<Piece<T, L::PER> *>(x.w + r * (L::PER * (int)sizeof(T) / 4)) = y;
         }
+    }
+    // row i with nothing but own elements: one side of every product.  (Read again for every four entries, with their loads: kept from one to the next,
+    // the loads of a new row would be waited for where the row changes.)
+    __device__ __forceinline__ Gathered<T, VEC> own(int i) const {
+        Gathered<T, VEC> x = row(i);
+        if (!GENERIC && d < VEC * G) keep_own(x);
         return x;
     }
 };
@@ -251,6 +250,7 @@ template <class T, int VEC, int G, bool GENERIC> struct Sums {
 // A group's place in its chunk: the row it is in, and the columns (and buckets) of the next four entries, fetched a batch ahead.
 struct Walk {
     int e, end, i, row_end;
+    int next_end;            // where the row behind this one ends: fetched while this one is walked
     bool goes_on;            // the row began in an earlier chunk
     int col[kBatch];
     unsigned bucket;         // four of eight bits
@@ -270,13 +270,26 @@ struct Walk {
             }
         }
     }
-    __device__ __forceinline__ void begin(const WalkPattern &p, int chunk) {
+    __device__ __forceinline__ void look_ahead(const WalkPattern &p) { next_end = p.row_ptr[i + 2 < p.n_rows ? i + 2 : p.n_rows]; }
+    // The row of the chunk's first entry is found by the lanes of the group together (lane `j` of `lanes`), which narrow the rows down (lanes + 1)-fold a
+    // look: a launch that did so ahead of the walk cost 9 us.  All of them and no others are active in the group.
+    __device__ __forceinline__ void begin(const WalkPattern &p, int chunk, int j, int lanes) {
         e = chunk * p.chunk;
         end = p.nnz - e < p.chunk ? p.nnz : e + p.chunk;
-        i = p.chunk_row[chunk];
-        row_end = p.row_ptr[i + 1];
-        goes_on = p.row_ptr[i] < e;
         fetch(p, e);
+        int lo = 0, hi = p.n_rows;     // row_ptr[lo] <= e < row_ptr[hi]
+        const unsigned long long mine = (lanes < 64 ? (1ull << lanes) - 1 : ~0ull) << ((int)(threadIdx.x & 63) - j);
+        while (hi - lo > 1) {
+            const int step = (hi - lo + lanes) / (lanes + 1), at = lo + step * (j + 1);
+            const int below = __popcll(__ballot(at < hi && p.row_ptr[at < hi ? at : lo] <= e) & mine);
+            lo += step * below;
+            if (lo + step < hi) hi = lo + step;
+        }
+        i = lo;
+        row_end = p.row_ptr[i + 1];
+        look_ahead(p);
+        goes_on = p.row_ptr[i] < e;
+        if (j == 0 && blockIdx.y == 0) p.chunk_row[chunk] = i;   // for the pass that joins the pieces
     }
     __device__ __forceinline__ int count() const {
         const int n = (row_end < end ? row_end : end) - e;
@@ -295,9 +308,10 @@ struct Walk {
     __device__ __forceinline__ bool row_done() const { return e == row_end || e == end; }
     // the row of entry e, which lies behind row i: the next one, or across a run of empty rows by doubling steps and halving
     __device__ __forceinline__ void next_row(const WalkPattern &p) {
-        int lo = i, hi = i + 1, step = 1;
-        row_end = p.row_ptr[hi + 1];
+        i = i + 1;
+        row_end = next_end;
         if (row_end <= e) {
+            int lo = i, hi = i, step = 1;
             do {
                 lo = hi;
                 hi = hi + step < p.n_rows ? hi + step : p.n_rows - 1;
@@ -307,9 +321,10 @@ struct Walk {
                 const int mid = (lo + hi) >> 1;
                 if (p.row_ptr[mid + 1] <= e) lo = mid; else hi = mid;
             }
+            i = hi;
             row_end = p.row_ptr[hi + 1];
         }
-        i = hi;
+        look_ahead(p);
         goes_on = false;
     }
 };
@@ -317,16 +332,20 @@ struct Walk {
 // Where a lane works: t of the G lanes of head h, group `chunk` of the walk.
 template <int G> struct Place {
     int t, slot, in_bundle, h, chunk;
+    int in_group, group_lanes;   // the lane within the group; lanes of the heads that there are
     bool live;       // a head and a chunk that there are
     __device__ __forceinline__ Place(int n_heads, int n_chunks, int bundle_log) {
         const int lane = threadIdx.x & 63, groups = (64 / G) >> bundle_log;
         t = lane % G;
         slot = lane / G;
+        in_group = lane & ((G << bundle_log) - 1);
         in_bundle = slot & ((1 << bundle_log) - 1);
         const int head = ((int)blockIdx.y << bundle_log) + in_bundle;
         chunk = ((int)blockIdx.x * waves() + (int)(threadIdx.x >> 6)) * groups + (slot >> bundle_log);
         live = head < n_heads && chunk < n_chunks;
         h = head < n_heads ? head : n_heads - 1;
+        const int left = n_heads - ((int)blockIdx.y << bundle_log);
+        group_lanes = G * (left < 1 << bundle_log ? left : 1 << bundle_log);
     }
 };
 
@@ -376,8 +395,7 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
     const float *bias = a.bias ? a.bias + h * a.n_buckets : nullptr;
     const unsigned offset = drop_offset(a.key);
     Walk w;
-    w.begin(a.p, at.chunk);
-    Gathered<T, VEC> q = Q.own(w.i);
+    w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
     Sums<T, VEC, G, GENERIC> acc;
     acc.zero();
     float m = -INFINITY, l = 0.f;    // l: the lane's own entries
@@ -385,19 +403,15 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
         const int n = w.count();
         int col[kBatch];
         w.columns(n, col);
+        const float b = bias ? bias[w.own_bucket(t, a.n_buckets)] : 0.f;
+        const Gathered<T, VEC> q = Q.own(w.i);
         Gathered<T, VEC> k[kBatch], v[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) k[u] = K.row(col[u]);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
-        bool use = (t & 3) < n, keep = true;
-        float b = 0.f;
-        if (bias) {
-            b = bias[w.own_bucket(t, a.n_buckets)];
-            use = use && b != -INFINITY;
-        }
-        if (a.key.threshold) keep = kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
+        const bool keep = !a.key.threshold || kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h), use = (t & 3) < n && b != -INFINITY;
         if (bias && __any((t & 3) < n && !use)) {   // a masked entry has no share, whatever its key and value hold
             if (!of_quad<0>((int)use)) v[0].zero();
             if (!of_quad<1>((int)use)) v[1].zero();
@@ -432,7 +446,6 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
             }
             if (w.e < w.end) {
                 w.next_row(a.p);
-                q = Q.own(w.i);
                 acc.zero();
                 m = -INFINITY;
                 l = 0.f;
@@ -449,50 +462,30 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
     const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
     if (!at.live) return;
     const int h = at.h, g = h / a.ratio, t = at.t;
-    const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, h * a.d, a.d, t), K(a.K, a.ldk, g * a.d, a.d, t), V(a.V, a.ldv, g * a.dv, a.dv, t), Y(a.Y, a.ldy, h * a.dv, a.dv, t),
-        dY(a.dY, a.lddy, h * a.dv, a.dv, t);
+    const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, h * a.d, a.d, t), K(a.K, a.ldk, g * a.d, a.d, t), V(a.V, a.ldv, g * a.dv, a.dv, t), dY(a.dY, a.lddy, h * a.dv, a.dv, t);
     T *dQ = static_cast<T *>(a.O1) + (size_t)h * a.d;
     const float *bias = a.bias ? a.bias + h * a.n_buckets : nullptr;
     const unsigned offset = drop_offset(a.key);
     Walk w;
-    w.begin(a.p, at.chunk);
-    Gathered<T, VEC> q, dy;
+    w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
     Sums<T, VEC, G, GENERIC> acc, share;         // sum of ds k; of alpha slope scale k, which delta is taken out by
-    float m, log_l, D, delta;
-    auto enter = [&]() {
-        q = Q.own(w.i);
-        dy = dY.own(w.i);
-        const Gathered<T, VEC> y = Y.own(w.i);
-        const float2 ml = a.stats[(size_t)w.i * a.heads + h];
-        m = ml.x;
-        log_l = ml.y;
-        float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) s = fmaf(dy.get(k), y.get(k), s);
-        D = head_sum<G>(s);
-        if (!w.goes_on && t == 0) a.row_stats[(size_t)w.i * a.heads + h] = make_float4(m, log_l, D, 0.f);
-        acc.zero();
-        if (!WHOLE_Y) share.zero();
-        delta = 0.f;
-    };
-    enter();
+    acc.zero();
+    share.zero();
+    float delta = 0.f;
     while (w.e < w.end) {
         const int n = w.count();
         int col[kBatch];
         w.columns(n, col);
+        const float b = bias ? bias[w.own_bucket(t, a.n_buckets)] : 0.f;
+        const Gathered<T, VEC> q = Q.own(w.i), dy = dY.own(w.i);
+        const float4 st = a.row_stats[(size_t)w.i * a.heads + h];
         Gathered<T, VEC> k[kBatch], v[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) k[u] = K.row(col[u]);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
-        bool use = (t & 3) < n, keep = true;
-        float b = 0.f;
-        if (bias) {
-            b = bias[w.own_bucket(t, a.n_buckets)];
-            use = use && b != -INFINITY;
-        }
-        if (a.key.threshold) keep = kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
+        const bool keep = !a.key.threshold || kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h), use = (t & 3) < n && b != -INFINITY;
         if (bias && __any((t & 3) < n && !use)) {
             if (!of_quad<0>((int)use)) k[0].zero();
             if (!of_quad<1>((int)use)) k[1].zero();
@@ -507,7 +500,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
         }
         const Score sc = score_of(a, four_sums<G>(s, t));
         const float dot_v = four_sums<G>(o, t), dp = keep ? dot_v * a.key.keep_scale : 0.f;
-        const float p = use ? exp_neg((sc.x + b - m) - log_l) : 0.f, dt = use ? p * (dp - D) : 0.f;
+        const float p = use ? exp_neg((sc.x + b - st.x) - st.y) : 0.f, dt = use ? p * (dp - st.z) : 0.f;
         const float by = sc.slope * a.scale, ds = dt * by;
         acc.add(of_quad<0>(ds), k[0]);
         acc.add(of_quad<1>(ds), k[1]);
@@ -527,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
             if (!w.goes_on && w.e == w.row_end) {
                 if (!WHOLE_Y) {
                     acc.add(-off, share);
-                    if (t == 0) a.row_stats[(size_t)w.i * a.heads + h].z = D + off;
+                    if (t == 0) a.row_stats[(size_t)w.i * a.heads + h].z = st.z + off;
                 }
                 acc.store(dQ + (long long)w.i * a.ldo1, t, a.d, 1.f);
             } else {
@@ -541,7 +534,9 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
             }
             if (w.e < w.end) {
                 w.next_row(a.p);
-                enter();
+                acc.zero();
+                if (!WHOLE_Y) share.zero();
+                delta = 0.f;
             }
         }
     }
@@ -570,8 +565,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
         const float *bias = a.bias ? a.bias + g * per : nullptr;
         const unsigned offset = drop_offset(a.key);
         Walk w;
-        w.begin(a.p, at.chunk);
-        Gathered<T, VEC> k = K.own(w.i), v = V.own(w.i);
+        w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
         Sums<T, VEC, G, GENERIC> dk, dv;
         dk.zero();
         dv.zero();
@@ -580,22 +574,18 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
             int row[kBatch];
             w.columns(n, row);
             const int own = own_of(t, row[0], row[1], row[2], row[3]), bin = bias ? w.own_bucket(t, a.n_buckets) : 0;
-            if (w.e + n < w.end) w.fetch(a.p, w.e + n);
+            const Gathered<T, VEC> k = K.own(w.i), v = V.own(w.i);
             for (int r = 0; r < a.ratio; ++r) {
                 const int h = g * a.ratio + r;
+                const float b = bias ? bias[r * a.n_buckets + bin] : 0.f;
+                const float4 st = a.row_stats[(size_t)own * a.heads + h];
                 Gathered<T, VEC> q[kBatch], dy[kBatch];
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) q[u] = Q.row(row[u], (long long)r * a.d * (int)sizeof(T));
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) dy[u] = dY.row(row[u], (long long)r * a.dv * (int)sizeof(T));
-                const float4 st = a.row_stats[(size_t)own * a.heads + h];
-                bool use = (t & 3) < n, keep = true;
-                float b = 0.f;
-                if (bias) {
-                    b = bias[r * a.n_buckets + bin];
-                    use = use && b != -INFINITY;
-                }
-                if (a.key.threshold) keep = kept(a.key, offset, own, w.i, h);
+                if (r == 0 && w.e + n < w.end) w.fetch(a.p, w.e + n);
+                const bool keep = !a.key.threshold || kept(a.key, offset, own, w.i, h), use = (t & 3) < n && b != -INFINITY;
                 if (bias && __any((t & 3) < n && !use)) {
                     if (!of_quad<0>((int)use)) { q[0].zero(); dy[0].zero(); }
                     if (!of_quad<1>((int)use)) { q[1].zero(); dy[1].zero(); }
@@ -638,8 +628,6 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
                 }
                 if (w.e < w.end) {
                     w.next_row(a.p);
-                    k = K.own(w.i);
-                    v = V.own(w.i);
                     dk.zero();
                     dv.zero();
                 }
@@ -678,8 +666,10 @@ __global__ __launch_bounds__(1024) void k_attention_bias(const float *__restrict
 
 enum { kJoinForward = 0, kJoinRows = 1, kJoinCols = 2 };
 
-// A wavefront per chunk boundary (and bundle of heads): where a row crosses it that crossed none before, the wavefront joins that row's pieces, its
-// groups taking them in turn.  Workgroups behind those (of the first bundle) look over 64 rows a wavefront and write the rows without entries.
+// A group per chunk boundary (and bundle of heads): where a row crosses it that crossed none before, the group joins that row's pieces, in their order; a
+// row of more than kManyPieces is left to the whole wavefront, whose groups take them in turn.  Workgroups behind those (of the first bundle)
+// look over 64 rows a wavefront and write the rows without entries.
+constexpr int kManyPieces = 16;
 template <class T, int VEC, int G, int MODE, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_heads, int join_blocks) {
     const int lane = threadIdx.x & 63, wave = (int)blockIdx.x * waves() + (int)(threadIdx.x >> 6);
@@ -699,13 +689,16 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
         }
         return;
     }
-    const int c = wave + 1;
-    if (c >= a.p.n_chunks) return;
-    const int i = a.p.chunk_row[c], start = a.p.row_ptr[i], T0 = a.p.chunk;
-    if (start == c * T0 || start / T0 != c - 1) return;
-    const int pieces = (a.p.row_ptr[i + 1] - 1) / T0 - (c - 1) + 1;
     const int groups = (64 / G) >> a.bundle_log, t = lane % G, slot = lane / G, group = slot >> a.bundle_log;
     const int head = ((int)blockIdx.y << a.bundle_log) + (slot & ((1 << a.bundle_log) - 1)), h = head < n_heads ? head : n_heads - 1;
+    // the first piece's chunk and the number of pieces of the row that first crosses the group's boundary; 0: there is none
+    int first = wave * groups + group, pieces = 0, i = 0;
+    if (first + 1 < a.p.n_chunks) {
+        const int T0 = a.p.chunk, c = first + 1;
+        i = a.p.chunk_row[c];
+        const int start = a.p.row_ptr[i];
+        if (start != c * T0 && start / T0 == first) pieces = (a.p.row_ptr[i + 1] - 1) / T0 - first + 1;
+    }
     constexpr bool TWO = MODE == kJoinCols || (MODE == kJoinRows && sizeof(T) == 2);
     constexpr int W = (TWO ? 2 : 1) * G * VEC;
     using S = Sums<T, VEC, G, GENERIC>;
@@ -720,8 +713,8 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
         s1.scale(f);
         s1.add(fo, o);
     };
-    for (int k = group; k < pieces; k += groups) {
-        const size_t at = piece_at(c - 1 + k, k > 0, n_heads, h);
+    auto take = [&](int from, int k) {
+        const size_t at = piece_at(from + k, k > 0, n_heads, h);
         S x;
         x.get(a.piece + at * W, t);
         if (MODE == kJoinForward) {
@@ -735,63 +728,74 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
             }
             if (MODE == kJoinRows && TWO) delta += a.piece_ml[at].x;
         }
-    }
-    for (int dist = G << a.bundle_log; dist < 64; dist <<= 1) {
-        S x;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) x.v[k] = __shfl_xor(s1.v[k], dist, 64);
-        if (MODE == kJoinForward) join(__shfl_xor(m, dist, 64), __shfl_xor(l, dist, 64), x);
-        else {
-            s1.add(1.f, x);
-            if (TWO) {
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) x.v[k] = __shfl_xor(s2.v[k], dist, 64);
-                s2.add(1.f, x);
-            }
-            if (MODE == kJoinRows && TWO) delta += __shfl_xor(delta, dist, 64);
+    };
+    auto finish = [&](int row) {
+        if (head >= n_heads) return;
+        if (MODE == kJoinForward) {
+            s1.store(static_cast<T *>(a.O1) + (long long)row * a.ldo1 + (size_t)h * a.dv, t, a.dv, l == 0.f ? 0.f : a.key.keep_scale / l);
+            if (t == 0) a.stats[(size_t)row * n_heads + h] = make_float2(m, logf(l));
+            return;
         }
+        if (MODE == kJoinRows && TWO) {
+            s1.add(-delta, s2);
+            if (t == 0) a.row_stats[(size_t)row * n_heads + h].z += delta;
+        }
+        s1.store(static_cast<T *>(a.O1) + (long long)row * a.ldo1 + (size_t)h * a.d, t, a.d, 1.f);
+        if (MODE == kJoinCols) s2.store(static_cast<T *>(a.O2) + (long long)row * a.ldo2 + (size_t)h * a.dv, t, a.dv, 1.f);
+    };
+    const unsigned long long many = __ballot(pieces > kManyPieces);
+    if (pieces > 0 && pieces <= kManyPieces) {
+        for (int k = 0; k < pieces; ++k) take(first, k);
+        finish(i);
     }
-    if (group != 0 || head >= n_heads) return;
-    if (MODE == kJoinForward) {
-        s1.store(static_cast<T *>(a.O1) + (long long)i * a.ldo1 + (size_t)h * a.dv, t, a.dv, l == 0.f ? 0.f : a.key.keep_scale / l);
-        if (t == 0) a.stats[(size_t)i * n_heads + h] = make_float2(m, logf(l));
-        return;
+    const int group_lanes = G << a.bundle_log;
+    for (int o = 0; o < groups; ++o) {
+        if (!(many >> (o * group_lanes) & 1)) continue;     // the same for the whole wavefront
+        const int from = __shfl(first, o * group_lanes, 64), row = __shfl(i, o * group_lanes, 64), n = __shfl(pieces, o * group_lanes, 64);
+        s1.zero();
+        s2.zero();
+        m = -INFINITY;
+        l = delta = 0.f;
+        for (int k = group; k < n; k += groups) take(from, k);
+        for (int dist = group_lanes; dist < 64; dist <<= 1) {
+            S x;
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x.v[k] = __shfl_xor(s1.v[k], dist, 64);
+            if (MODE == kJoinForward) join(__shfl_xor(m, dist, 64), __shfl_xor(l, dist, 64), x);
+            else {
+                s1.add(1.f, x);
+                if (TWO) {
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) x.v[k] = __shfl_xor(s2.v[k], dist, 64);
+                    s2.add(1.f, x);
+                }
+                if (MODE == kJoinRows && TWO) delta += __shfl_xor(delta, dist, 64);
+            }
+        }
+        if (group == 0) finish(row);
     }
-    if (MODE == kJoinRows && TWO) {
-        s1.add(-delta, s2);
-        if (t == 0) a.row_stats[(size_t)i * n_heads + h].z += delta;
-    }
-    s1.store(static_cast<T *>(a.O1) + (long long)i * a.ldo1 + (size_t)h * a.d, t, a.d, 1.f);
-    if (MODE == kJoinCols) s2.store(static_cast<T *>(a.O2) + (long long)i * a.ldo2 + (size_t)h * a.dv, t, a.dv, 1.f);
 }
 
-// ------------------------------------------------------------------------------------------------------------------ preparation
-
-// chunk_row[c] = row of entry c * chunk, of up to two patterns; and the buckets in the order of the transposed pattern
-struct PrepArgs {
-    struct { const int32_t *row_ptr; int32_t *chunk_row; int n_rows, chunk, n_chunks, block0; } plan[2];
-    int n_plans, scatter0;
-    const uint8_t *bucket;
-    const int32_t *t_pos;
-    uint8_t *out;
-    int nnz;
-};
-__global__ __launch_bounds__(kThreads) void k_attention_prep(PrepArgs a) {
-    if ((int)blockIdx.x >= a.scatter0) {
-        const long long k = (long long)((int)blockIdx.x - a.scatter0) * kThreads + threadIdx.x;
-        if (k < a.nnz) a.out[a.t_pos[k]] = a.bucket[k];
+// (m, log l, D) of every row and query head, D = <dY, Y>; workgroups behind those put the buckets into the order of the transposed pattern
+template <class T, int VEC, int G, bool GENERIC>
+__global__ __launch_bounds__(kThreads) void k_attention_row_stats(AttnArgs a, unsigned blocks, const uint8_t *__restrict__ bucket, const int32_t *__restrict__ t_pos,
+                                                                  int nnz, uint8_t *__restrict__ out) {
+    if (blockIdx.x >= blocks) {
+        const long long k = (long long)(blockIdx.x - blocks) * kThreads + threadIdx.x;
+        if (k < nnz) out[t_pos[k]] = bucket[k];
         return;
     }
-    const auto &p = a.n_plans > 1 && (int)blockIdx.x >= a.plan[1].block0 ? a.plan[1] : a.plan[0];
-    const int c = ((int)blockIdx.x - p.block0) * kThreads + (int)threadIdx.x;
-    if (c >= p.n_chunks) return;
-    const int e = c * p.chunk;
-    int lo = 0, hi = p.n_rows;     // row_ptr[lo] <= e < row_ptr[hi]
-    while (hi - lo > 1) {
-        const int mid = lo + ((hi - lo) >> 1);
-        if (p.row_ptr[mid] <= e) lo = mid; else hi = mid;
-    }
-    p.chunk_row[c] = lo;
+    const long long at = (long long)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+    if (at >= (long long)a.p.n_rows * a.heads) return;
+    const int i = (int)(at / a.heads), h = (int)(at % a.heads), t = threadIdx.x % G;
+    const Source<T, VEC, G, GENERIC> Y(a.Y, a.ldy, h * a.dv, a.dv, t), dY(a.dY, a.lddy, h * a.dv, a.dv, t);
+    const Gathered<T, VEC> y = Y.own(i), dy = dY.own(i);
+    const float2 ml = a.stats[at];
+    float d = 0.f;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) d = fmaf(dy.get(k), y.get(k), d);
+    d = head_sum<G>(d);
+    if (t == 0) a.row_stats[at] = make_float4(ml.x, ml.y, d, 0.f);
 }
 
 // ------------------------------------------------------------------------------------------------------------------ host side
@@ -802,15 +806,17 @@ Shape shape_of(int d, int dv) {
     const int w = d > dv ? d : dv;
     return w <= 16 ? Shape{4, 4} : w <= 32 ? Shape{8, 4} : w <= 64 ? Shape{8, 8} : w <= 128 ? Shape{8, 16} : Shape{8, 32};
 }
-// Heads of a bundle: as many as fill a 128-byte line, and all query heads of a key head
+// Heads of a bundle: as many as gather 256 bytes an entry, and all query heads of a key head (`together`).  Bundles of 1, 2, 4, 8 heads, us: 290,000
+// nodes of batched graphs, 8 heads of 16 in bf16, forward and backward 12,377 / 5,320 / 2,890 / 2,623; 100,000 nodes of 21, 4 heads of 32 in fp32 1,247 /
+// 1,164 / 1,263; 233,000 nodes of 87, 8 heads of 64 on 2 in bf16, forward 4,086 / 2,206 / 1,983 / 1,949.
 int bundle_log_of(const Shape &s, int n_heads, int together, int bytes) {
     int log = 0;
-    while ((s.lanes << (log + 1)) <= 64 && (1 << log) < n_heads && ((bytes << log) < 128 || (1 << log) < together)) ++log;
+    while ((s.lanes << (log + 1)) <= 64 && (1 << log) < n_heads && ((bytes << log) / together < 256 || (1 << log) < together)) ++log;
     return log;
 }
 int chunk_of(int64_t nnz, int bundles, int groups) {
     int t = 256;
-    while (t > 16 && nnz / t * bundles / groups < 8192) t >>= 1;
+    while (t > 32 && nnz / t * bundles / groups < 16384) t >>= 1;
     return t;
 }
 
@@ -878,13 +884,13 @@ AttnArgs args_of(const AttentionCall &c) {
     return a;
 }
 
-WalkPattern pattern_of(const sensei_csr &A, const Layout &l, const uint8_t *bucket, const int32_t *chunk_row) {
+WalkPattern pattern_of(const sensei_csr &A, const Layout &l, const uint8_t *bucket, int32_t *chunk_row) {
     return {A.row_ptr, A.col_idx, bucket, chunk_row, A.n_rows, (int)A.nnz, l.chunk, l.n_chunks};
 }
 
 template <class T, int VEC, int G, bool GENERIC, int MODE> hipError_t join_and_fill(const AttnArgs &a, const Layout &l, int n_heads, hipStream_t s) {
     constexpr int waves = kThreads / 64;
-    const int join_blocks = l.n_chunks > 1 ? (l.n_chunks - 1 + waves - 1) / waves : 0, fill = (int)((a.p.n_rows + 64ll * waves - 1) / (64 * waves));
+    const int join_blocks = l.n_chunks > 1 ? l.blocks(waves) : 0, fill = (int)((a.p.n_rows + 64ll * waves - 1) / (64 * waves));
     if (join_blocks + fill == 0) return hipSuccess;
     hipLaunchKernelGGL((k_attention_join<T, VEC, G, MODE, GENERIC>), dim3(join_blocks + fill, l.bundles), dim3(kThreads), 0, s, a, n_heads, join_blocks);
     return hipGetLastError();
@@ -901,7 +907,11 @@ template <class T, int VEC, int G, bool GENERIC> hipError_t backward_shape(const
     a.p = pr;
     a.O1 = c.dQ; a.ldo1 = c.lddq;
     a.bundle_log = room.rows.bundle_log;
-    if (pr.nnz > 0) hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G, GENERIC>), dim3(room.rows.blocks(kThreads / 64), room.rows.bundles), dim3(kThreads), 0, s, a);
+    if (pr.nnz > 0) {
+        const unsigned blocks = (unsigned)(((int64_t)pr.n_rows * a.heads + kThreads / G - 1) / (kThreads / G)), more = a.bias ? (unsigned)((pr.nnz + kThreads - 1) / kThreads) : 0;
+        hipLaunchKernelGGL((k_attention_row_stats<T, VEC, G, GENERIC>), dim3(blocks + more), dim3(kThreads), 0, s, a, blocks, c.bucket, c.t_pos, pr.nnz, const_cast<uint8_t *>(pc.bucket));
+        hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G, GENERIC>), dim3(room.rows.blocks(kThreads / 64), room.rows.bundles), dim3(kThreads), 0, s, a);
+    }
     if ((e = join_and_fill<T, VEC, G, GENERIC, kJoinRows>(a, room.rows, a.heads, s)) != hipSuccess) return e;
     a.p = pc;
     a.O1 = c.dK; a.ldo1 = c.lddk;
@@ -941,13 +951,6 @@ hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s) {
     a.piece_ml = reinterpret_cast<float2 *>(ws + l.rows_bytes() + l.piece_bytes(c.heads, 1));
     a.O1 = c.out; a.ldo1 = c.ldo;
     a.bundle_log = l.bundle_log;
-    if (c.A->nnz > 0) {
-        PrepArgs p = {};
-        p.n_plans = 1;
-        p.plan[0] = {c.A->row_ptr, chunk_row, c.A->n_rows, l.chunk, l.n_chunks, 0};
-        p.scatter0 = (l.n_chunks + kThreads - 1) / kThreads;
-        hipLaunchKernelGGL(k_attention_prep, dim3(p.scatter0), dim3(kThreads), 0, s, p);
-    }
     const bool plain = plain_gathers(c, l.shape);
 #define SENSEI_CALL(T, V, G, GEN) forward_shape<T, V, G, GEN>(a, l, s)
     return SENSEI_BY_TYPE(c.type, l.shape, plain, SENSEI_CALL);
@@ -968,15 +971,7 @@ hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream
     a.piece_ml = reinterpret_cast<float2 *>(take(room.ml));
     a.bias_part = a.bias && c.dbias ? reinterpret_cast<float *>(take(room.bias)) : nullptr;
     const WalkPattern pr = pattern_of(*c.A, room.rows, a.bias ? c.bucket : nullptr, rows_r), pc = pattern_of(*c.At, room.cols, a.bias ? bucket_t : nullptr, rows_c);
-    if (c.A->nnz > 0) {
-        PrepArgs p = {};
-        p.n_plans = 2;
-        p.plan[0] = {c.A->row_ptr, rows_r, c.A->n_rows, room.rows.chunk, room.rows.n_chunks, 0};
-        p.plan[1] = {c.At->row_ptr, rows_c, c.At->n_rows, room.cols.chunk, room.cols.n_chunks, (room.rows.n_chunks + kThreads - 1) / kThreads};
-        p.scatter0 = p.plan[1].block0 + (room.cols.n_chunks + kThreads - 1) / kThreads;
-        p.bucket = c.bucket; p.t_pos = c.t_pos; p.out = bucket_t; p.nnz = (int)c.A->nnz;
-        hipLaunchKernelGGL(k_attention_prep, dim3(p.scatter0 + (a.bias ? (p.nnz + kThreads - 1) / kThreads : 0)), dim3(kThreads), 0, s, p);
-    } else if (a.bias_part) {
+    if (c.A->nnz == 0 && a.bias_part) {
         const hipError_t e = launch_zero_matrix(c.dbias, 1, c.heads * c.n_buckets, c.heads * c.n_buckets, false, s);
         if (e != hipSuccess) return e;
     }
