@@ -3078,8 +3078,9 @@ int sensei_attention_backward_workspace(const sensei_csr *A, const sensei_attent
     if (!csr_ok(A, false) || !attention_opts_ok(opts, d_k, d_v) || type < SENSEI_F32 || type > SENSEI_F16 || !bytes) return SENSEI_INVALID_ARGUMENT;
     AttentionCall c = attention_call(A, *opts, d_k, d_v, type);
     float with_gradient;
-    c.dbias = &with_gradient;   // room for it, wanted or not
-    *bytes = attention_backward_ws_bytes(c);
+    const size_t without = attention_backward_ws_bytes(c);   // room for both, whether the bias' gradient is wanted or not
+    c.dbias = &with_gradient;
+    *bytes = std::max(without, attention_backward_ws_bytes(c));
     return SENSEI_OK;
 }
 

@@ -11,12 +11,12 @@
 // and dbias is summed by the walk over the columns, which has the whole D.
 //
 // What bounds these walks is the gathering of k and v (q and dy) rows from the caches, and behind it the instructions around four operations an
-// element.  A head's vector is spread over G lanes, eight elements (four for heads of at most 16) a lane; a group of lanes takes the same
-// entry for a few neighbouring heads (a bundle), so that a gather takes whole 128-byte lines and shared key heads are read once; and every group
-// walks a chunk of consecutive entries by itself, four at a time.  The four dot products are summed so that every lane of a quad ends up
-// with one of them: cap, bias, mask, exponential and generator are worked out once an entry and head (not in every lane), and the
-// weights are handed round by moves within the quad.  Rows that cross chunks leave a piece per chunk in scratch, joined by a second kernel
-// in chunk order: results do not depend on scheduling.
+// element.  A head's vector is spread over as few lanes as hold 32 bytes of it each (G: one lane for 16 elements of 16 bits); a group of lanes takes
+// the same entry for a few neighbouring heads (a bundle), so that a gather takes whole 128-byte lines and shared key heads are read
+// once; and every group walks a chunk of consecutive entries by itself, four at a time (a batch).  The four dot products are summed so that
+// the lanes of a head share them out: cap, bias, mask and exponential are worked out once an entry and head, and the weights are handed
+// round by moves within a quad of lanes; so are the generator's words, of which a call has four heads'.  Rows that cross chunks leave a
+// piece per chunk in scratch, joined by a second kernel in chunk order: results do not depend on scheduling.
 #include "element_types.h"
 #include "sensei_internal.h"
 
@@ -59,42 +59,82 @@ template <int CTRL> __device__ __forceinline__ int dpp(int x) { return __builtin
 
 __device__ __forceinline__ float from_16_away(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
 
-// sum over the four lanes of a quad, in all of them
-__device__ __forceinline__ float quad_sum(float x) {
-    x += dpp<0xB1>(x);          // the neighbour in a pair
-    return x + dpp<0x4E>(x);    // the other pair
-}
 // sum over the G lanes of a head, in all of them (the lanes of a head are always active together)
 template <int G> __device__ __forceinline__ float head_sum(float x) {
-    x = quad_sum(x);
+    if (G >= 2) x += dpp<0xB1>(x);           // the neighbour in a pair
+    if (G >= 4) x += dpp<0x4E>(x);           // the other pair of a quad
     if (G >= 8) x += dpp<0x141>(x);          // mirrored within eight lanes
     if (G >= 16) x += dpp<0x140>(x);         // mirrored within sixteen
     if (G >= 32) x += from_16_away(x);
     return x;
 }
-// four sums over the G lanes of a head at once, sum t % 4 in lane t
-template <int G> __device__ __forceinline__ float four_sums(const float (&s)[4], int t) {
-    float a0 = s[0], a1 = s[1], a2 = s[2], a3 = s[3];
-    if (G == 8) {
-        a0 += dpp<0x141>(a0); a1 += dpp<0x141>(a1); a2 += dpp<0x141>(a2); a3 += dpp<0x141>(a3);
+
+// What a head's lanes work out for the four entries of a batch: lane t has entry t % 4, with two lanes a head entries t and t + 2, a lone lane all.
+template <int G> struct Own {
+    static constexpr int N = G >= 4 ? 1 : 4 / G, SHARERS = G < 4 ? G : 4;
+    __device__ __forceinline__ static int entry(int t, int o) { return G >= 4 ? t & 3 : t + G * o; }
+    __device__ __forceinline__ static int of(int t, int o, const int (&x)[kBatch]) {
+        if (G == 1) return x[o];
+        if (G == 2) {
+            const int even = x[2 * o], odd = x[2 * o + 1];
+            return t ? odd : even;
+        }
+        const int x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3], lo = t & 1 ? x1 : x0, hi = t & 1 ? x3 : x2;
+        return t & 2 ? hi : lo;
     }
-    const bool odd = t & 1, high = t & 2;
-    float lo = odd ? a1 : a0, hi = odd ? a3 : a2;
-    lo += dpp<0xB1>(odd ? a0 : a1);
-    hi += dpp<0xB1>(odd ? a2 : a3);
-    float x = high ? hi : lo;
-    x += dpp<0x4E>(high ? lo : hi);
-    if (G >= 16) {      // quads of a row of sixteen lanes, turned by one and by two
-        x += dpp<0x124>(x);
-        x += dpp<0x128>(x);
+    // sums over the head's lanes of four numbers, each to the lane whose it is
+    __device__ __forceinline__ static void sums(const float (&s)[kBatch], int t, float (&out)[N]) {
+        if constexpr (G == 1) {
+#pragma unroll
+            for (int o = 0; o < 4; ++o) out[o] = s[o];
+        } else if constexpr (G == 2) {
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const float even = s[2 * o], odd = s[2 * o + 1];
+                out[o] = (t ? odd : even) + dpp<0xB1>(t ? even : odd);
+            }
+        } else {
+            float a0 = s[0], a1 = s[1], a2 = s[2], a3 = s[3];
+            if (G == 8) {
+                a0 += dpp<0x141>(a0); a1 += dpp<0x141>(a1); a2 += dpp<0x141>(a2); a3 += dpp<0x141>(a3);
+            }
+            const bool odd = t & 1, high = t & 2;
+            float lo = odd ? a1 : a0, hi = odd ? a3 : a2;
+            lo += dpp<0xB1>(odd ? a0 : a1);
+            hi += dpp<0xB1>(odd ? a2 : a3);
+            float x = high ? hi : lo;
+            x += dpp<0x4E>(high ? lo : hi);
+            if (G >= 16) {      // quads of a row of sixteen lanes, turned by one and by two
+                x += dpp<0x124>(x);
+                x += dpp<0x128>(x);
+            }
+            if (G >= 32) x += from_16_away(x);
+            out[0] = x;
+        }
     }
-    if (G >= 32) x += from_16_away(x);
+    // entry U's number, in all lanes of the head
+    template <int U, class X> __device__ __forceinline__ static X get(const X (&own)[N]) {
+        if constexpr (G == 1) return own[U];
+        else if constexpr (G == 2) return dpp<U & 1 ? 0xF5 : 0xA0>(own[U / 2]);
+        else return dpp<U * 0x55>(own[0]);
+    }
+    // the largest of the four, the sum of what every lane has for its own
+    __device__ __forceinline__ static float max(const float (&own)[N]) {
+        float x = own[0];
+#pragma unroll
+        for (int o = 1; o < N; ++o) x = fmaxf(x, own[o]);
+        if (G >= 2) x = fmaxf(x, dpp<0xB1>(x));
+        if (G >= 4) x = fmaxf(x, dpp<0x4E>(x));
+        return x;
+    }
+    __device__ __forceinline__ static float sum(float x) { return head_sum<SHARERS>(x); }
+};
+
+// The number as it is, but worked on here: what follows from it is not kept from outside a loop in registers that are short there.
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
     return x;
 }
-// what lane U of the quad holds
-template <int U> __device__ __forceinline__ float of_quad(float x) { return dpp<U * 0x55>(x); }
-template <int U> __device__ __forceinline__ int of_quad(int x) { return dpp<U * 0x55>(x); }
-__device__ __forceinline__ int own_of(int t, int x0, int x1, int x2, int x3) { return t & 2 ? (t & 1 ? x3 : x2) : (t & 1 ? x1 : x0); }
 
 // A lane's share of a head's vector of d elements: PIECES pieces of PER, piece r from element at(r) = (r G + t) PER on, so that the lanes of a head read
 // side by side.  Where the vector ends inside a piece the lane reads the last PER elements instead and leaves those before at(r) to the lane
@@ -110,9 +150,9 @@ template <class T, int VEC, int G, bool GENERIC> struct Lanes {
 template <class T, int VEC> struct Gathered {
     static constexpr int WORDS = VEC * (int)sizeof(T) / 4;
     unsigned w[WORDS];
-    __device__ __forceinline__ void zero() {
+    __device__ __forceinline__ void mask(int ones) {
 #pragma unroll
-        for (int k = 0; k < WORDS; ++k) w[k] = 0u;
+        for (int k = 0; k < WORDS; ++k) w[k] &= (unsigned)ones;
     }
     __device__ __forceinline__ float get(int k) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
@@ -177,6 +217,7 @@ template <class T, int VEC, int G, bool GENERIC> struct Source {
     }
     // 0 in the place of elements that are not this lane's own
     __device__ __forceinline__ void keep_own(Gathered<T, VEC> &x) const {
+        const int t = here(this->t);
 #pragma unroll
         for (int r = 0; r < L::PIECES; ++r) {
             const int skip = L::at(r, t) - L::from(r, t, d);   // of the piece's elements; a lane behind the end has none
@@ -216,7 +257,8 @@ template <class T, int VEC, int G, bool GENERIC> struct Sums {
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v[k] *= w;
     }
-    __device__ __forceinline__ void store(T *p, int t, int d, float by) const {
+    __device__ __forceinline__ void store(T *p, int t_, int d, float by) const {
+        const int t = here(t_);
 #pragma unroll
         for (int r = 0; r < L::PIECES; ++r) {
             const int first = L::at(r, t), from = L::from(r, t, d);
@@ -271,8 +313,8 @@ struct Walk {
         }
     }
     __device__ __forceinline__ void look_ahead(const WalkPattern &p) { next_end = p.row_ptr[i + 2 < p.n_rows ? i + 2 : p.n_rows]; }
-    // The row of the chunk's first entry is found by the lanes of the group together (lane `j` of `lanes`), which narrow the rows down (lanes + 1)-fold a
-    // look: a launch that did so ahead of the walk cost 9 us.  All of them and no others are active in the group.
+    // The row of the chunk's first entry is found by the group's lanes together (lane `j` of `lanes`), which narrow the rows down (4 lanes + 1)-fold a
+    // look: a launch that did so ahead of the walk cost 9 us.
     __device__ __forceinline__ void begin(const WalkPattern &p, int chunk, int j, int lanes) {
         e = chunk * p.chunk;
         end = p.nnz - e < p.chunk ? p.nnz : e + p.chunk;
@@ -280,8 +322,13 @@ struct Walk {
         int lo = 0, hi = p.n_rows;     // row_ptr[lo] <= e < row_ptr[hi]
         const unsigned long long mine = (lanes < 64 ? (1ull << lanes) - 1 : ~0ull) << ((int)(threadIdx.x & 63) - j);
         while (hi - lo > 1) {
-            const int step = (hi - lo + lanes) / (lanes + 1), at = lo + step * (j + 1);
-            const int below = __popcll(__ballot(at < hi && p.row_ptr[at < hi ? at : lo] <= e) & mine);
+            const int step = (hi - lo + 4 * lanes) / (4 * lanes + 1);
+            int below = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const long long at = lo + (long long)step * (4 * j + q + 1);
+                below += __popcll(__ballot(at < hi && p.row_ptr[at < hi ? at : lo] <= e) & mine);
+            }
             lo += step * below;
             if (lo + step < hi) hi = lo + step;
         }
@@ -301,8 +348,8 @@ struct Walk {
 #pragma unroll
         for (int u = 1; u < kBatch; ++u) c[u] = u < n ? col[u] : col[0];
     }
-    __device__ __forceinline__ int own_bucket(int t, int n_buckets) const {
-        const int b = (int)(bucket >> (8 * (t & 3)) & 255u);
+    __device__ __forceinline__ int bucket_of(int u, int n_buckets) const {
+        const int b = (int)(bucket >> (8 * u) & 255u);
         return b < n_buckets ? b : n_buckets - 1;
     }
     __device__ __forceinline__ bool row_done() const { return e == row_end || e == end; }
@@ -329,23 +376,24 @@ struct Walk {
     }
 };
 
-// Where a lane works: t of the G lanes of head h, group `chunk` of the walk.
+// Where a lane works: t of the G lanes of head h, group `chunk` of the walk.  The lanes of a bundle's heads that there are not work along on the last
+// head (others want what they work out) and store nothing.
 template <int G> struct Place {
     int t, slot, in_bundle, h, chunk;
-    int in_group, group_lanes;   // the lane within the group; lanes of the heads that there are
-    bool live;       // a head and a chunk that there are
+    int in_group, group_lanes;
+    bool live, head_live;
     __device__ __forceinline__ Place(int n_heads, int n_chunks, int bundle_log) {
         const int lane = threadIdx.x & 63, groups = (64 / G) >> bundle_log;
         t = lane % G;
         slot = lane / G;
-        in_group = lane & ((G << bundle_log) - 1);
+        group_lanes = G << bundle_log;
+        in_group = lane & (group_lanes - 1);
         in_bundle = slot & ((1 << bundle_log) - 1);
         const int head = ((int)blockIdx.y << bundle_log) + in_bundle;
         chunk = ((int)blockIdx.x * waves() + (int)(threadIdx.x >> 6)) * groups + (slot >> bundle_log);
-        live = head < n_heads && chunk < n_chunks;
-        h = head < n_heads ? head : n_heads - 1;
-        const int left = n_heads - ((int)blockIdx.y << bundle_log);
-        group_lanes = G * (left < 1 << bundle_log ? left : 1 << bundle_log);
+        live = chunk < n_chunks;
+        head_live = head < n_heads;
+        h = head_live ? head : n_heads - 1;
     }
 };
 
@@ -372,11 +420,53 @@ __device__ __forceinline__ Score score_of(const AttnArgs &a, float dot) {
     return {a.cap * th.value, th.slope};
 }
 
-// does the weight of entry (row, col) stay for query head h?
-__device__ __forceinline__ bool kept(const DropKey &key, unsigned offset, int row, int col, int h) {
-    const Words w = philox((unsigned)col, (unsigned)row, 0x80000000u | (unsigned)(h >> 2), offset, key.k0, key.k1);
-    const unsigned w0 = w.w[0], w1 = w.w[1], w2 = w.w[2], w3 = w.w[3];
-    return (h & 2 ? (h & 1 ? w3 : w2) : (h & 1 ? w1 : w0)) >= key.threshold;
+// Which weights of the lane's own entries stay for query head h: generator at counter (column, row, 2^31 + h / 4, offset), word h % 4.  COLS: the entries
+// lie in one column, else in one row.  A lane calls it for its own entries; where lanes of one quad work on the same entries for heads of
+// one call (bundles of neighbouring heads, fewer than four lanes a head), each calls it for other entries and hands round four bits.
+template <int G, bool COLS>
+__device__ __forceinline__ void kept(const DropKey &key, unsigned offset, int fixed, const int (&other)[kBatch], int h, int t, int bundle_log, bool (&keep)[Own<G>::N]) {
+    using O = Own<G>;
+    auto words = [&](int x) {
+        return COLS ? philox((unsigned)fixed, (unsigned)x, 0x80000000u | (unsigned)(h >> 2), offset, key.k0, key.k1)
+                    : philox((unsigned)x, (unsigned)fixed, 0x80000000u | (unsigned)(h >> 2), offset, key.k0, key.k1);
+    };
+    auto mine = [&](int x) {
+        const Words w = words(x);
+        const unsigned w0 = w.w[0], w1 = w.w[1], w2 = w.w[2], w3 = w.w[3], lo = h & 1 ? w1 : w0, hi = h & 1 ? w3 : w2;
+        return (h & 2 ? hi : lo) >= key.threshold;
+    };
+    auto bits = [&](int x) {
+        const Words w = words(x);
+        return (w.w[0] >= key.threshold ? 1 : 0) | (w.w[1] >= key.threshold ? 2 : 0) | (w.w[2] >= key.threshold ? 4 : 0) | (w.w[3] >= key.threshold ? 8 : 0);
+    };
+    if constexpr (G < 4) {
+        const int z = threadIdx.x & 3;
+        if ((G << bundle_log) >= 4) {
+            const int b = bits(Own<4>::of(z, 0, other));
+            if constexpr (G == 2) {
+                keep[0] = dpp<0x44>(b) >> (h & 3) & 1;
+                keep[1] = dpp<0xEE>(b) >> (h & 3) & 1;
+            } else {
+                keep[0] = dpp<0x00>(b) >> (h & 3) & 1;
+                keep[1] = dpp<0x55>(b) >> (h & 3) & 1;
+                keep[2] = dpp<0xAA>(b) >> (h & 3) & 1;
+                keep[3] = dpp<0xFF>(b) >> (h & 3) & 1;
+            }
+            return;
+        }
+        if constexpr (G == 1) {
+            if (bundle_log == 1) {
+                const int b0 = bits(Own<2>::of(z & 1, 0, other)), b1 = bits(Own<2>::of(z & 1, 1, other));
+                keep[0] = dpp<0xA0>(b0) >> (h & 3) & 1;
+                keep[1] = dpp<0xF5>(b0) >> (h & 3) & 1;
+                keep[2] = dpp<0xA0>(b1) >> (h & 3) & 1;
+                keep[3] = dpp<0xF5>(b1) >> (h & 3) & 1;
+                return;
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < O::N; ++o) keep[o] = mine(O::of(t, o, other));
 }
 __device__ __forceinline__ unsigned drop_offset(const DropKey &key) { return key.offset + (key.offset_dev ? *key.offset_dev : 0u); }
 
@@ -385,8 +475,12 @@ __device__ __forceinline__ size_t piece_at(int chunk, bool goes_on, int heads, i
 
 // ------------------------------------------------------------------------------------------------------------------ forward
 
+// entry U of a batch: its gathered numbers are wiped where it is masked (a masked entry has no share, whatever it holds)
+#define SENSEI_EACH(F) F(0) F(1) F(2) F(3)
+
 template <class T, int VEC, int G, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
+    using O = Own<G>;
     const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
     if (!at.live) return;
     const int h = at.h, g = h / a.ratio, t = at.t;
@@ -403,7 +497,9 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
         const int n = w.count();
         int col[kBatch];
         w.columns(n, col);
-        const float b = bias ? bias[w.own_bucket(t, a.n_buckets)] : 0.f;
+        float b[O::N];
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) b[o] = bias ? bias[w.bucket_of(O::entry(t, o), a.n_buckets)] : 0.f;
         const Gathered<T, VEC> q = Q.own(w.i);
         Gathered<T, VEC> k[kBatch], v[kBatch];
 #pragma unroll
@@ -411,38 +507,55 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-        const bool keep = !a.key.threshold || kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h), use = (t & 3) < n && b != -INFINITY;
-        if (bias && __any((t & 3) < n && !use)) {   // a masked entry has no share, whatever its key and value hold
-            if (!of_quad<0>((int)use)) v[0].zero();
-            if (!of_quad<1>((int)use)) v[1].zero();
-            if (!of_quad<2>((int)use)) v[2].zero();
-            if (!of_quad<3>((int)use)) v[3].zero();
+        bool keep[O::N];
+        if (a.key.threshold) kept<G, false>(a.key, offset, w.i, col, h, t, a.bundle_log, keep);
+        int use[O::N];               // all ones, or none
+        bool masked = false;
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) {
+            const bool there = O::entry(t, o) < n, open = b[o] != -INFINITY;
+            use[o] = there && open ? -1 : 0;
+            masked = masked || (there && !open);
         }
-        float s[kBatch];
+        if (bias && __any(masked)) {
+#define SENSEI_WIPE(U) v[U].mask(O::template get<U>(use));
+            SENSEI_EACH(SENSEI_WIPE)
+#undef SENSEI_WIPE
+        }
+        float s[kBatch], x[O::N];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) s[u] = dot(q, k[u]);
-        const Score sc = score_of(a, four_sums<G>(s, t));   // every lane takes part, whatever its entry
-        const float x = use ? sc.x + b : -INFINITY;
-        float top = fmaxf(x, dpp<0xB1>(x));
-        top = fmaxf(m, fmaxf(top, dpp<0x4E>(top)));
-        const float base = top > -INFINITY ? top : 0.f, f = exp_neg(m - base), p = exp_neg(x - base), kp = keep ? p : 0.f;
+        O::sums(s, t, x);
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) {
+            const float y = score_of(a, x[o]).x + b[o];
+            x[o] = use[o] ? y : -INFINITY;
+        }
+        const float top = fmaxf(m, O::max(x)), base = top > -INFINITY ? top : 0.f, f = exp_neg(m - base);
         m = top;
-        l = fmaf(l, f, p);
+        l *= f;
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) {
+            const float p = exp_neg(x[o] - base);
+            l += p;
+            x[o] = a.key.threshold && !keep[o] ? 0.f : p;
+        }
         acc.scale(f);
-        acc.add(of_quad<0>(kp), v[0]);
-        acc.add(of_quad<1>(kp), v[1]);
-        acc.add(of_quad<2>(kp), v[2]);
-        acc.add(of_quad<3>(kp), v[3]);
+#define SENSEI_ADD(U) acc.add(O::template get<U>(x), v[U]);
+        SENSEI_EACH(SENSEI_ADD)
+#undef SENSEI_ADD
         w.e += n;
         if (w.row_done()) {
-            const float sum = quad_sum(l);
-            if (!w.goes_on && w.e == w.row_end) {
-                acc.store(Y + (long long)w.i * a.ldo1, t, a.dv, sum == 0.f ? 0.f : a.key.keep_scale / sum);
-                if (t == 0) a.stats[(size_t)w.i * a.heads + h] = make_float2(m, logf(sum));
-            } else {
-                const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
-                acc.put(a.piece + at_piece * (G * VEC), t);
-                if (t == 0) a.piece_ml[at_piece] = make_float2(m, sum);
+            const float sum = O::sum(l);
+            if (at.head_live) {
+                if (!w.goes_on && w.e == w.row_end) {
+                    acc.store(Y + (long long)w.i * a.ldo1, t, a.dv, sum == 0.f ? 0.f : a.key.keep_scale / sum);
+                    if (t == 0) a.stats[(size_t)w.i * a.heads + h] = make_float2(m, logf(sum));
+                } else {
+                    const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
+                    acc.put(a.piece + at_piece * (G * VEC), t);
+                    if (t == 0) a.piece_ml[at_piece] = make_float2(m, sum);
+                }
             }
             if (w.e < w.end) {
                 w.next_row(a.p);
@@ -459,6 +572,7 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
 template <class T, int VEC, int G, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
     constexpr bool WHOLE_Y = sizeof(T) == 4;     // Y holds what D needs
+    using O = Own<G>;
     const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
     if (!at.live) return;
     const int h = at.h, g = h / a.ratio, t = at.t;
@@ -476,7 +590,9 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
         const int n = w.count();
         int col[kBatch];
         w.columns(n, col);
-        const float b = bias ? bias[w.own_bucket(t, a.n_buckets)] : 0.f;
+        float b[O::N];
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) b[o] = bias ? bias[w.bucket_of(O::entry(t, o), a.n_buckets)] : 0.f;
         const Gathered<T, VEC> q = Q.own(w.i), dy = dY.own(w.i);
         const float4 st = a.row_stats[(size_t)w.i * a.heads + h];
         Gathered<T, VEC> k[kBatch], v[kBatch];
@@ -485,51 +601,62 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-        const bool keep = !a.key.threshold || kept(a.key, offset, w.i, own_of(t, col[0], col[1], col[2], col[3]), h), use = (t & 3) < n && b != -INFINITY;
-        if (bias && __any((t & 3) < n && !use)) {
-            if (!of_quad<0>((int)use)) k[0].zero();
-            if (!of_quad<1>((int)use)) k[1].zero();
-            if (!of_quad<2>((int)use)) k[2].zero();
-            if (!of_quad<3>((int)use)) k[3].zero();
+        bool keep[O::N];
+        if (a.key.threshold) kept<G, false>(a.key, offset, w.i, col, h, t, a.bundle_log, keep);
+        int use[O::N];
+        bool masked = false;
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) {
+            const bool there = O::entry(t, o) < n, open = b[o] != -INFINITY;
+            use[o] = there && open ? -1 : 0;
+            masked = masked || (there && !open);
         }
-        float s[kBatch], o[kBatch];
+        if (bias && __any(masked)) {
+#define SENSEI_WIPE(U) k[U].mask(O::template get<U>(use));
+            SENSEI_EACH(SENSEI_WIPE)
+#undef SENSEI_WIPE
+        }
+        float s[kBatch], c[kBatch], x[O::N], dv[O::N];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             s[u] = dot(q, k[u]);
-            o[u] = dot(dy, v[u]);
+            c[u] = dot(dy, v[u]);
         }
-        const Score sc = score_of(a, four_sums<G>(s, t));
-        const float dot_v = four_sums<G>(o, t), dp = keep ? dot_v * a.key.keep_scale : 0.f;
-        const float p = use ? exp_neg((sc.x + b - st.x) - st.y) : 0.f, dt = use ? p * (dp - st.z) : 0.f;
-        const float by = sc.slope * a.scale, ds = dt * by;
-        acc.add(of_quad<0>(ds), k[0]);
-        acc.add(of_quad<1>(ds), k[1]);
-        acc.add(of_quad<2>(ds), k[2]);
-        acc.add(of_quad<3>(ds), k[3]);
-        if (!WHOLE_Y) {
+        O::sums(s, t, x);
+        O::sums(c, t, dv);
+        float pb[O::N];
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) {
+            const Score sc = score_of(a, x[o]);
+            const float dp = a.key.threshold && !keep[o] ? 0.f : dv[o] * a.key.keep_scale;
+            const float p = use[o] ? exp_neg((sc.x + b[o] - st.x) - st.y) : 0.f, dt = use[o] ? p * (dp - st.z) : 0.f, by = sc.slope * a.scale;
             delta += dt;
-            const float pb = p * by;
-            share.add(of_quad<0>(pb), k[0]);
-            share.add(of_quad<1>(pb), k[1]);
-            share.add(of_quad<2>(pb), k[2]);
-            share.add(of_quad<3>(pb), k[3]);
+            x[o] = dt * by;
+            pb[o] = p * by;
         }
+#define SENSEI_ADD(U)                                                 \
+    acc.add(O::template get<U>(x), k[U]);                             \
+    if constexpr (!WHOLE_Y) share.add(O::template get<U>(pb), k[U]);
+        SENSEI_EACH(SENSEI_ADD)
+#undef SENSEI_ADD
         w.e += n;
         if (w.row_done()) {
-            const float off = WHOLE_Y ? 0.f : quad_sum(delta);
-            if (!w.goes_on && w.e == w.row_end) {
-                if (!WHOLE_Y) {
-                    acc.add(-off, share);
-                    if (t == 0) a.row_stats[(size_t)w.i * a.heads + h].z = st.z + off;
-                }
-                acc.store(dQ + (long long)w.i * a.ldo1, t, a.d, 1.f);
-            } else {
-                const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
-                float *to = a.piece + at_piece * ((WHOLE_Y ? 1 : 2) * G * VEC);
-                acc.put(to, t);
-                if (!WHOLE_Y) {
-                    share.put(to + G * VEC, t);
-                    if (t == 0) a.piece_ml[at_piece] = make_float2(off, 0.f);
+            const float off = WHOLE_Y ? 0.f : O::sum(delta);
+            if (at.head_live) {
+                if (!w.goes_on && w.e == w.row_end) {
+                    if (!WHOLE_Y) {
+                        acc.add(-off, share);
+                        if (t == 0) a.row_stats[(size_t)w.i * a.heads + h].z = st.z + off;
+                    }
+                    acc.store(dQ + (long long)w.i * a.ldo1, t, a.d, 1.f);
+                } else {
+                    const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
+                    float *to = a.piece + at_piece * ((WHOLE_Y ? 1 : 2) * G * VEC);
+                    acc.put(to, t);
+                    if (!WHOLE_Y) {
+                        share.put(to + G * VEC, t);
+                        if (t == 0) a.piece_ml[at_piece] = make_float2(off, 0.f);
+                    }
                 }
             }
             if (w.e < w.end) {
@@ -550,6 +677,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
 template <class T, int VEC, int G, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
     extern __shared__ float tables[];
+    using O = Own<G>;
     const Place<G> at(a.kv_heads, a.p.n_chunks, a.bundle_log);
     const int per = a.ratio * a.n_buckets;
     float *table = tables + ((int)(threadIdx.x >> 6) * (64 / G) + at.slot) * per;
@@ -564,6 +692,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
         T *dK = static_cast<T *>(a.O1) + (size_t)g * a.d, *dV = static_cast<T *>(a.O2) + (size_t)g * a.dv;
         const float *bias = a.bias ? a.bias + g * per : nullptr;
         const unsigned offset = drop_offset(a.key);
+        const int call_log = a.ratio == 1 ? a.bundle_log : 0;   // heads of one generator call lie side by side
         Walk w;
         w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
         Sums<T, VEC, G, GENERIC> dk, dv;
@@ -571,60 +700,84 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
         dv.zero();
         while (w.e < w.end) {
             const int n = w.count();
-            int row[kBatch];
+            int row[kBatch], own[O::N], bin[O::N];
             w.columns(n, row);
-            const int own = own_of(t, row[0], row[1], row[2], row[3]), bin = bias ? w.own_bucket(t, a.n_buckets) : 0;
+#pragma unroll
+            for (int o = 0; o < O::N; ++o) {
+                own[o] = O::of(t, o, row);
+                bin[o] = bias ? w.bucket_of(O::entry(t, o), a.n_buckets) : 0;
+            }
             const Gathered<T, VEC> k = K.own(w.i), v = V.own(w.i);
             for (int r = 0; r < a.ratio; ++r) {
                 const int h = g * a.ratio + r;
-                const float b = bias ? bias[r * a.n_buckets + bin] : 0.f;
-                const float4 st = a.row_stats[(size_t)own * a.heads + h];
+                float b[O::N];
+                float4 st[O::N];
+#pragma unroll
+                for (int o = 0; o < O::N; ++o) {
+                    b[o] = bias ? bias[r * a.n_buckets + bin[o]] : 0.f;
+                    st[o] = a.row_stats[(size_t)own[o] * a.heads + h];
+                }
                 Gathered<T, VEC> q[kBatch], dy[kBatch];
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) q[u] = Q.row(row[u], (long long)r * a.d * (int)sizeof(T));
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) dy[u] = dY.row(row[u], (long long)r * a.dv * (int)sizeof(T));
                 if (r == 0 && w.e + n < w.end) w.fetch(a.p, w.e + n);
-                const bool keep = !a.key.threshold || kept(a.key, offset, own, w.i, h), use = (t & 3) < n && b != -INFINITY;
-                if (bias && __any((t & 3) < n && !use)) {
-                    if (!of_quad<0>((int)use)) { q[0].zero(); dy[0].zero(); }
-                    if (!of_quad<1>((int)use)) { q[1].zero(); dy[1].zero(); }
-                    if (!of_quad<2>((int)use)) { q[2].zero(); dy[2].zero(); }
-                    if (!of_quad<3>((int)use)) { q[3].zero(); dy[3].zero(); }
+                bool keep[O::N];
+                if (a.key.threshold) kept<G, true>(a.key, offset, w.i, row, h, t, call_log, keep);
+                int use[O::N];
+                bool masked = false;
+#pragma unroll
+                for (int o = 0; o < O::N; ++o) {
+                    const bool there = O::entry(t, o) < n, open = b[o] != -INFINITY;
+                    use[o] = there && open ? -1 : 0;
+                    masked = masked || (there && !open);
                 }
-                float s[kBatch], o[kBatch];
+                if (bias && __any(masked)) {
+#define SENSEI_WIPE(U)                     \
+    q[U].mask(O::template get<U>(use));    \
+    dy[U].mask(O::template get<U>(use));
+                    SENSEI_EACH(SENSEI_WIPE)
+#undef SENSEI_WIPE
+                }
+                float s[kBatch], c[kBatch], x[O::N], pw[O::N];
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
                     s[u] = dot(k, q[u]);
-                    o[u] = dot(v, dy[u]);
+                    c[u] = dot(v, dy[u]);
                 }
-                const Score sc = score_of(a, four_sums<G>(s, t));
-                const float dot_v = four_sums<G>(o, t), dp = keep ? dot_v * a.key.keep_scale : 0.f;
-                const float p = use ? exp_neg((sc.x + b - st.x) - st.y) : 0.f, dt = use ? p * (dp - st.z) : 0.f;
-                const float ds = dt * sc.slope * a.scale, pw = keep ? p * a.key.keep_scale : 0.f;
-                if (a.bias_part) {   // one lane after the other: two of a quad may be in one bucket
+                O::sums(s, t, x);
+                O::sums(c, t, pw);
 #pragma unroll
-                    for (int u = 0; u < kBatch; ++u)
-                        if (t == u && use) __hip_atomic_fetch_add(table + r * a.n_buckets + bin, dt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                for (int o = 0; o < O::N; ++o) {
+                    const Score sc = score_of(a, x[o]);
+                    const float ks = a.key.threshold && !keep[o] ? 0.f : a.key.keep_scale, dp = ks == 0.f ? 0.f : pw[o] * ks;
+                    const float p = use[o] ? exp_neg((sc.x + b[o] - st[o].x) - st[o].y) : 0.f, dt = use[o] ? p * (dp - st[o].z) : 0.f;
+                    x[o] = dt * sc.slope * a.scale;
+                    pw[o] = p * ks;
+                    if (a.bias_part) {   // a head's lanes one after the other: two may be in one bucket
+#pragma unroll
+                        for (int z = 0; z < O::SHARERS; ++z)
+                            if (t == z && use[o]) __hip_atomic_fetch_add(table + r * a.n_buckets + bin[o], dt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
                 }
-                dk.add(of_quad<0>(ds), q[0]);
-                dk.add(of_quad<1>(ds), q[1]);
-                dk.add(of_quad<2>(ds), q[2]);
-                dk.add(of_quad<3>(ds), q[3]);
-                dv.add(of_quad<0>(pw), dy[0]);
-                dv.add(of_quad<1>(pw), dy[1]);
-                dv.add(of_quad<2>(pw), dy[2]);
-                dv.add(of_quad<3>(pw), dy[3]);
+#define SENSEI_ADD(U)                      \
+    dk.add(O::template get<U>(x), q[U]);   \
+    dv.add(O::template get<U>(pw), dy[U]);
+                SENSEI_EACH(SENSEI_ADD)
+#undef SENSEI_ADD
             }
             w.e += n;
             if (w.row_done()) {
-                if (!w.goes_on && w.e == w.row_end) {
-                    dk.store(dK + (long long)w.i * a.ldo1, t, a.d, 1.f);
-                    dv.store(dV + (long long)w.i * a.ldo2, t, a.dv, 1.f);
-                } else {
-                    float *to = a.piece + piece_at(at.chunk, w.goes_on, a.kv_heads, g) * (2 * G * VEC);
-                    dk.put(to, t);
-                    dv.put(to + G * VEC, t);
+                if (at.head_live) {
+                    if (!w.goes_on && w.e == w.row_end) {
+                        dk.store(dK + (long long)w.i * a.ldo1, t, a.d, 1.f);
+                        dv.store(dV + (long long)w.i * a.ldo2, t, a.dv, 1.f);
+                    } else {
+                        float *to = a.piece + piece_at(at.chunk, w.goes_on, a.kv_heads, g) * (2 * G * VEC);
+                        dk.put(to, t);
+                        dv.put(to + G * VEC, t);
+                    }
                 }
                 if (w.e < w.end) {
                     w.next_row(a.p);
@@ -800,11 +953,14 @@ __global__ __launch_bounds__(kThreads) void k_attention_row_stats(AttnArgs a, un
 
 // ------------------------------------------------------------------------------------------------------------------ host side
 
-// Lanes of a head and elements a lane, from the wider of a head's key and value.
+// Lanes of a head, from the wider of a head's key and value: 32 bytes a lane.  Tables of dbias (`table` floats a head) are kept for every head that a
+// wavefront works on: more lanes a head where those would not fit 64 KB.
 struct Shape { int vec, lanes; };
-Shape shape_of(int d, int dv) {
+Shape shape_of(int d, int dv, int elem, int table) {
     const int w = d > dv ? d : dv;
-    return w <= 16 ? Shape{4, 4} : w <= 32 ? Shape{8, 4} : w <= 64 ? Shape{8, 8} : w <= 128 ? Shape{8, 16} : Shape{8, 32};
+    Shape s{32 / elem, 1};
+    while (s.lanes * s.vec < w || (size_t)(64 / s.lanes) * table * sizeof(float) > 65536) s.lanes *= 2;
+    return s;
 }
 // Heads of a bundle: as many as gather 256 bytes an entry, and all query heads of a key head (`together`).  Bundles of 1, 2, 4, 8 heads, us: 290,000
 // nodes of batched graphs, 8 heads of 16 in bf16, forward and backward 12,377 / 5,320 / 2,890 / 2,623; 100,000 nodes of 21, 4 heads of 32 in fp32 1,247 /
@@ -823,8 +979,10 @@ int chunk_of(int64_t nnz, int bundles, int groups) {
 struct Layout {
     Shape shape;
     int bundle_log, bundles, groups, chunk, n_chunks;
-    Layout(int64_t nnz, int n_heads, int together, int d, int dv, int elem) {
-        shape = shape_of(d, dv);
+    Layout(const AttentionCall &c, bool cols) {
+        const int64_t nnz = c.A->nnz;
+        const int n_heads = cols ? c.kv_heads : c.heads, together = cols ? 1 : c.heads / c.kv_heads, elem = c.elem, d = c.d, dv = c.dv;
+        shape = shape_of(d, dv, elem, c.dbias ? c.heads / c.kv_heads * c.n_buckets : 0);
         bundle_log = bundle_log_of(shape, n_heads, together, (d > dv ? d : dv) * elem);
         bundles = (n_heads + (1 << bundle_log) - 1) >> bundle_log;
         groups = (64 / shape.lanes) >> bundle_log;
@@ -848,7 +1006,7 @@ struct Room {   // what the backward carves its scratch into
     int col_waves;
     size_t bucket, stats, piece, ml, bias;
     Room(const AttentionCall &c)
-        : rows(c.A->nnz, c.heads, c.heads / c.kv_heads, c.d, c.dv, c.elem), cols(c.A->nnz, c.kv_heads, 1, c.d, c.dv, c.elem) {
+        : rows(c, false), cols(c, true) {
         col_waves = table_waves(c, cols.shape);
         bucket = c.n_buckets > 0 ? align_up((size_t)c.A->nnz, 256) : 0;
         stats = align_up((size_t)c.A->n_rows * c.heads * sizeof(float4), 256);
@@ -863,7 +1021,7 @@ struct Room {   // what the backward carves its scratch into
 // Gathers by 24-bit products and 32-bit offsets, whole pieces: every number of a row and of bytes a row below 2^24, every matrix below 4 GB, heads
 // no narrower than a piece.
 bool plain_gathers(const AttentionCall &c, const Shape &s) {
-    const int per = s.vec < 16 / c.elem ? s.vec : 16 / c.elem;
+    const int per = 16 / c.elem;
     if (c.d < per || c.dv < per || c.A->n_rows >= 1 << 24 || c.A->n_cols >= 1 << 24) return false;
     struct { int64_t rows, ld; } m[] = {{c.A->n_cols, c.ldk}, {c.A->n_cols, c.ldv}, {c.At ? c.A->n_rows : 0, c.ldq}, {c.At ? c.A->n_rows : 0, c.lddy}};
     for (const auto &x : m)
@@ -926,24 +1084,24 @@ template <class T, int VEC, int G, bool GENERIC> hipError_t backward_shape(const
     return join_and_fill<T, VEC, G, GENERIC, kJoinCols>(a, room.cols, a.kv_heads, s);
 }
 
-#define SENSEI_BY_SHAPE(T, shape, GEN, CALL)                                                                        \
-    (shape.vec == 4 ? CALL(T, 4, 4, GEN) : shape.lanes == 4 ? CALL(T, 8, 4, GEN) : shape.lanes == 8 ? CALL(T, 8, 8, GEN) \
-     : shape.lanes == 16 ? CALL(T, 8, 16, GEN) : CALL(T, 8, 32, GEN))
-#define SENSEI_BY_GATHER(T, shape, plain, CALL) (plain ? SENSEI_BY_SHAPE(T, shape, false, CALL) : SENSEI_BY_SHAPE(T, shape, true, CALL))
-#define SENSEI_BY_TYPE(type, shape, plain, CALL)                                                                  \
-    (type == SENSEI_F32 ? SENSEI_BY_GATHER(float, shape, plain, CALL) : type == SENSEI_BF16 ? SENSEI_BY_GATHER(Bf16, shape, plain, CALL) \
-     : SENSEI_BY_GATHER(F16, shape, plain, CALL))
+#define SENSEI_BY_SHAPE(T, VEC, lanes, GEN, CALL)                                                              \
+    (lanes == 1 ? CALL(T, VEC, 1, GEN) : lanes == 2 ? CALL(T, VEC, 2, GEN) : lanes == 4 ? CALL(T, VEC, 4, GEN) \
+     : lanes == 8 ? CALL(T, VEC, 8, GEN) : lanes == 16 ? CALL(T, VEC, 16, GEN) : CALL(T, VEC, 32, GEN))
+#define SENSEI_BY_GATHER(T, VEC, lanes, plain, CALL) (plain ? SENSEI_BY_SHAPE(T, VEC, lanes, false, CALL) : SENSEI_BY_SHAPE(T, VEC, lanes, true, CALL))
+#define SENSEI_BY_TYPE(type, lanes, plain, CALL)                                                                             \
+    (type == SENSEI_F32 ? SENSEI_BY_GATHER(float, 8, lanes, plain, CALL) : type == SENSEI_BF16 ? SENSEI_BY_GATHER(Bf16, 16, lanes, plain, CALL) \
+     : SENSEI_BY_GATHER(F16, 16, lanes, plain, CALL))
 
 }  // namespace
 
 size_t attention_ws_bytes(const AttentionCall &c) {
-    const Layout l(c.A->nnz, c.heads, c.heads / c.kv_heads, c.d, c.dv, c.elem);
+    const Layout l(c, false);
     return l.rows_bytes() + l.piece_bytes(c.heads, 1) + l.ml_bytes(c.heads) + 256;
 }
 
 hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s) {
     if (c.A->n_rows <= 0) return hipSuccess;
-    const Layout l(c.A->nnz, c.heads, c.heads / c.kv_heads, c.d, c.dv, c.elem);
+    const Layout l(c, false);
     AttnArgs a = args_of(c);
     int32_t *chunk_row = reinterpret_cast<int32_t *>(ws);
     a.p = pattern_of(*c.A, l, a.bias ? c.bucket : nullptr, chunk_row);
@@ -953,7 +1111,7 @@ hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s) {
     a.bundle_log = l.bundle_log;
     const bool plain = plain_gathers(c, l.shape);
 #define SENSEI_CALL(T, V, G, GEN) forward_shape<T, V, G, GEN>(a, l, s)
-    return SENSEI_BY_TYPE(c.type, l.shape, plain, SENSEI_CALL);
+    return SENSEI_BY_TYPE(c.type, l.shape.lanes, plain, SENSEI_CALL);
 #undef SENSEI_CALL
 }
 
@@ -977,7 +1135,7 @@ hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream
     }
     const bool plain = plain_gathers(c, room.rows.shape);
 #define SENSEI_CALL(T, V, G, GEN) backward_shape<T, V, G, GEN>(c, a, room, pr, pc, s)
-    return SENSEI_BY_TYPE(c.type, room.rows.shape, plain, SENSEI_CALL);
+    return SENSEI_BY_TYPE(c.type, room.rows.shape.lanes, plain, SENSEI_CALL);
 #undef SENSEI_CALL
 }
 
