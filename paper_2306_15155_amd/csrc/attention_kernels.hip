@@ -217,6 +217,7 @@ template <class T, int VEC, int G, bool GENERIC> struct Source {
     }
     // 0 in the place of elements that are not this lane's own
     __device__ __forceinline__ void keep_own(Gathered<T, VEC> &x) const {
+        if (GENERIC || d == VEC * G) return;
         const int t = here(this->t);
 #pragma unroll
         for (int r = 0; r < L::PIECES; ++r) {
@@ -228,11 +229,10 @@ template <class T, int VEC, int G, bool GENERIC> struct Source {
             }
         }
     }
-    // row i with nothing but own elements: one side of every product.  (Read again for every four entries, with their loads: kept from one to the next,
-    // the loads of a new row would be waited for where the row changes.)
+    // row i with nothing but own elements: one side of every product
     __device__ __forceinline__ Gathered<T, VEC> own(int i) const {
         Gathered<T, VEC> x = row(i);
-        if (!GENERIC && d < VEC * G) keep_own(x);
+        keep_own(x);
         return x;
     }
 };
@@ -248,6 +248,11 @@ template <class T, int VEC, int G, bool GENERIC> struct Sums {
     __device__ __forceinline__ void add(float w, const Gathered<T, VEC> &x) {
 #pragma unroll
         for (int k = 0; k < VEC; ++k) v[k] = fmaf(w, x.get(k), v[k]);
+    }
+    // nothing of x where `ones` is 0: a masked entry has no share, whatever its key and value hold
+    __device__ __forceinline__ void add(float w, Gathered<T, VEC> x, int ones) {
+        x.mask(ones);
+        add(w, x);
     }
     __device__ __forceinline__ void add(float w, const Sums &x) {
 #pragma unroll
@@ -423,8 +428,9 @@ __device__ __forceinline__ Score score_of(const AttnArgs &a, float dot) {
 // Which weights of the lane's own entries stay for query head h: generator at counter (column, row, 2^31 + h / 4, offset), word h % 4.  COLS: the entries
 // lie in one column, else in one row.  A lane calls it for its own entries; where lanes of one quad work on the same entries for heads of
 // one call (bundles of neighbouring heads, fewer than four lanes a head), each calls it for other entries and hands round four bits.
-template <int G, bool COLS>
-__device__ __forceinline__ void kept(const DropKey &key, unsigned offset, int fixed, const int (&other)[kBatch], int h, int t, int bundle_log, bool (&keep)[Own<G>::N]) {
+// Bit r of keep: head h + r, of the R heads (of one call) that the lane works on.
+template <int G, bool COLS, int R>
+__device__ __forceinline__ void kept(const DropKey &key, unsigned offset, int fixed, const int (&other)[kBatch], int h, int t, int bundle_log, int (&keep)[Own<G>::N]) {
     using O = Own<G>;
     auto words = [&](int x) {
         return COLS ? philox((unsigned)fixed, (unsigned)x, 0x80000000u | (unsigned)(h >> 2), offset, key.k0, key.k1)
@@ -439,6 +445,11 @@ __device__ __forceinline__ void kept(const DropKey &key, unsigned offset, int fi
         const Words w = words(x);
         return (w.w[0] >= key.threshold ? 1 : 0) | (w.w[1] >= key.threshold ? 2 : 0) | (w.w[2] >= key.threshold ? 4 : 0) | (w.w[3] >= key.threshold ? 8 : 0);
     };
+    if constexpr (R > 1) {
+#pragma unroll
+        for (int o = 0; o < O::N; ++o) keep[o] = bits(O::of(t, o, other)) >> (h & 3);
+        return;
+    }
     if constexpr (G < 4) {
         const int z = threadIdx.x & 3;
         if ((G << bundle_log) >= 4) {
@@ -466,7 +477,7 @@ __device__ __forceinline__ void kept(const DropKey &key, unsigned offset, int fi
         }
     }
 #pragma unroll
-    for (int o = 0; o < O::N; ++o) keep[o] = mine(O::of(t, o, other));
+    for (int o = 0; o < O::N; ++o) keep[o] = mine(O::of(t, o, other)) ? 1 : 0;
 }
 __device__ __forceinline__ unsigned drop_offset(const DropKey &key) { return key.offset + (key.offset_dev ? *key.offset_dev : 0u); }
 
@@ -475,196 +486,247 @@ __device__ __forceinline__ size_t piece_at(int chunk, bool goes_on, int heads, i
 
 // ------------------------------------------------------------------------------------------------------------------ forward
 
-// entry U of a batch: its gathered numbers are wiped where it is masked (a masked entry has no share, whatever it holds)
+// for every entry of a batch
 #define SENSEI_EACH(F) F(0) F(1) F(2) F(3)
 
-template <class T, int VEC, int G, bool GENERIC>
+// R: query heads of one key head that a lane takes together (R divides their number), from one gathering of the entry
+template <class T, int VEC, int G, bool GENERIC, int R>
 __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
     using O = Own<G>;
-    const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
+    const Place<G> at(a.heads / R, a.p.n_chunks, a.bundle_log);
     if (!at.live) return;
-    const int h = at.h, g = h / a.ratio, t = at.t;
+    const int h = at.h * R, g = h / a.ratio, t = at.t;
     const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, h * a.d, a.d, t), K(a.K, a.ldk, g * a.d, a.d, t), V(a.V, a.ldv, g * a.dv, a.dv, t);
     T *Y = static_cast<T *>(a.O1) + (size_t)h * a.dv;
     const float *bias = a.bias ? a.bias + h * a.n_buckets : nullptr;
     const unsigned offset = drop_offset(a.key);
     Walk w;
     w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
-    Sums<T, VEC, G, GENERIC> acc;
-    acc.zero();
-    float m = -INFINITY, l = 0.f;    // l: the lane's own entries
+    Gathered<T, VEC> q[R];
+    Sums<T, VEC, G, GENERIC> acc[R];
+    float m[R], l[R];                // l: the lane's own entries
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        acc[r].zero();
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+    }
+    bool fresh = true;
     while (w.e < w.end) {
         const int n = w.count();
-        int col[kBatch];
+        int col[kBatch], bin[O::N];
         w.columns(n, col);
-        float b[O::N];
+        float b[R][O::N];
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) b[o] = bias ? bias[w.bucket_of(O::entry(t, o), a.n_buckets)] : 0.f;
-        const Gathered<T, VEC> q = Q.own(w.i);
+        for (int o = 0; o < O::N; ++o) bin[o] = bias ? w.bucket_of(O::entry(t, o), a.n_buckets) : 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int o = 0; o < O::N; ++o) b[r][o] = bias ? bias[r * a.n_buckets + bin[o]] : 0.f;
+        if (fresh) {     // a new row's loads go with those of its first entries: waited for where the row changes, they cost a round trip a row
+#pragma unroll
+            for (int r = 0; r < R; ++r) q[r] = Q.row(w.i, (long long)r * a.d * (int)sizeof(T));
+            fresh = false;
+        }
         Gathered<T, VEC> k[kBatch], v[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) k[u] = K.row(col[u]);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-        bool keep[O::N];
-        if (a.key.threshold) kept<G, false>(a.key, offset, w.i, col, h, t, a.bundle_log, keep);
-        int use[O::N];               // all ones, or none
-        bool masked = false;
+        int keep[O::N];              // bit r: head h + r
+        if (a.key.threshold) kept<G, false, R>(a.key, offset, w.i, col, h, t, a.bundle_log, keep);
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) {
-            const bool there = O::entry(t, o) < n, open = b[o] != -INFINITY;
-            use[o] = there && open ? -1 : 0;
-            masked = masked || (there && !open);
-        }
-        if (bias && __any(masked)) {
-#define SENSEI_WIPE(U) v[U].mask(O::template get<U>(use));
-            SENSEI_EACH(SENSEI_WIPE)
-#undef SENSEI_WIPE
-        }
-        float s[kBatch], x[O::N];
+        for (int r = 0; r < R; ++r) {
+            Q.keep_own(q[r]);
+            int use[O::N];               // all ones, or none
+            bool masked = false;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) s[u] = dot(q, k[u]);
-        O::sums(s, t, x);
+            for (int o = 0; o < O::N; ++o) {
+                const bool there = O::entry(t, o) < n, open = b[r][o] != -INFINITY;
+                use[o] = there && open ? -1 : 0;
+                masked = masked || (there && !open);
+            }
+            float s[kBatch], x[O::N];
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) {
-            const float y = score_of(a, x[o]).x + b[o];
-            x[o] = use[o] ? y : -INFINITY;
-        }
-        const float top = fmaxf(m, O::max(x)), base = top > -INFINITY ? top : 0.f, f = exp_neg(m - base);
-        m = top;
-        l *= f;
+            for (int u = 0; u < kBatch; ++u) s[u] = dot(q[r], k[u]);
+            O::sums(s, t, x);
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) {
-            const float p = exp_neg(x[o] - base);
-            l += p;
-            x[o] = a.key.threshold && !keep[o] ? 0.f : p;
-        }
-        acc.scale(f);
-#define SENSEI_ADD(U) acc.add(O::template get<U>(x), v[U]);
-        SENSEI_EACH(SENSEI_ADD)
+            for (int o = 0; o < O::N; ++o) {
+                const float y = score_of(a, x[o]).x + b[r][o];
+                x[o] = use[o] ? y : -INFINITY;
+            }
+            const float top = fmaxf(m[r], O::max(x)), base = top > -INFINITY ? top : 0.f, f = exp_neg(m[r] - base);
+            m[r] = top;
+            l[r] *= f;
+#pragma unroll
+            for (int o = 0; o < O::N; ++o) {
+                const float p = exp_neg(x[o] - base);
+                l[r] += p;
+                x[o] = a.key.threshold && !(keep[o] >> r & 1) ? 0.f : p;
+            }
+            acc[r].scale(f);
+            if (bias && __any(masked)) {
+#define SENSEI_ADD(U) acc[r].add(O::template get<U>(x), v[U], O::template get<U>(use));
+                SENSEI_EACH(SENSEI_ADD)
 #undef SENSEI_ADD
+            } else {
+#define SENSEI_ADD(U) acc[r].add(O::template get<U>(x), v[U]);
+                SENSEI_EACH(SENSEI_ADD)
+#undef SENSEI_ADD
+            }
+        }
         w.e += n;
         if (w.row_done()) {
-            const float sum = O::sum(l);
-            if (at.head_live) {
-                if (!w.goes_on && w.e == w.row_end) {
-                    acc.store(Y + (long long)w.i * a.ldo1, t, a.dv, sum == 0.f ? 0.f : a.key.keep_scale / sum);
-                    if (t == 0) a.stats[(size_t)w.i * a.heads + h] = make_float2(m, logf(sum));
-                } else {
-                    const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
-                    acc.put(a.piece + at_piece * (G * VEC), t);
-                    if (t == 0) a.piece_ml[at_piece] = make_float2(m, sum);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float sum = O::sum(l[r]);
+                if (at.head_live) {
+                    if (!w.goes_on && w.e == w.row_end) {
+                        acc[r].store(Y + (long long)w.i * a.ldo1 + r * a.dv, t, a.dv, sum == 0.f ? 0.f : a.key.keep_scale / sum);
+                        if (t == 0) a.stats[(size_t)w.i * a.heads + h + r] = make_float2(m[r], logf(sum));
+                    } else {
+                        const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h + r);
+                        acc[r].put(a.piece + at_piece * (G * VEC), t);
+                        if (t == 0) a.piece_ml[at_piece] = make_float2(m[r], sum);
+                    }
                 }
+                acc[r].zero();
+                m[r] = -INFINITY;
+                l[r] = 0.f;
             }
-            if (w.e < w.end) {
-                w.next_row(a.p);
-                acc.zero();
-                m = -INFINITY;
-                l = 0.f;
-            }
+            if (w.e < w.end) w.next_row(a.p);
+            fresh = true;
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------------ backward, over the rows
 
-template <class T, int VEC, int G, bool GENERIC>
+template <class T, int VEC, int G, bool GENERIC, int R>
 __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
     constexpr bool WHOLE_Y = sizeof(T) == 4;     // Y holds what D needs
     using O = Own<G>;
-    const Place<G> at(a.heads, a.p.n_chunks, a.bundle_log);
+    const Place<G> at(a.heads / R, a.p.n_chunks, a.bundle_log);
     if (!at.live) return;
-    const int h = at.h, g = h / a.ratio, t = at.t;
+    const int h = at.h * R, g = h / a.ratio, t = at.t;
     const Source<T, VEC, G, GENERIC> Q(a.Q, a.ldq, h * a.d, a.d, t), K(a.K, a.ldk, g * a.d, a.d, t), V(a.V, a.ldv, g * a.dv, a.dv, t), dY(a.dY, a.lddy, h * a.dv, a.dv, t);
     T *dQ = static_cast<T *>(a.O1) + (size_t)h * a.d;
     const float *bias = a.bias ? a.bias + h * a.n_buckets : nullptr;
     const unsigned offset = drop_offset(a.key);
     Walk w;
     w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
-    Sums<T, VEC, G, GENERIC> acc, share;         // sum of ds k; of alpha slope scale k, which delta is taken out by
-    acc.zero();
-    share.zero();
-    float delta = 0.f;
+    Gathered<T, VEC> q[R], dy[R];
+    Sums<T, VEC, G, GENERIC> acc[R], share[R];   // sum of ds k; of alpha slope scale k, which delta is taken out by
+    float4 st[R];
+    float delta[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        acc[r].zero();
+        share[r].zero();
+        delta[r] = 0.f;
+    }
+    bool fresh = true;
     while (w.e < w.end) {
         const int n = w.count();
-        int col[kBatch];
+        int col[kBatch], bin[O::N];
         w.columns(n, col);
-        float b[O::N];
+        float b[R][O::N];
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) b[o] = bias ? bias[w.bucket_of(O::entry(t, o), a.n_buckets)] : 0.f;
-        const Gathered<T, VEC> q = Q.own(w.i), dy = dY.own(w.i);
-        const float4 st = a.row_stats[(size_t)w.i * a.heads + h];
+        for (int o = 0; o < O::N; ++o) bin[o] = bias ? w.bucket_of(O::entry(t, o), a.n_buckets) : 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int o = 0; o < O::N; ++o) b[r][o] = bias ? bias[r * a.n_buckets + bin[o]] : 0.f;
+        if (fresh) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                q[r] = Q.row(w.i, (long long)r * a.d * (int)sizeof(T));
+                dy[r] = dY.row(w.i, (long long)r * a.dv * (int)sizeof(T));
+                st[r] = a.row_stats[(size_t)w.i * a.heads + h + r];
+            }
+            fresh = false;
+        }
         Gathered<T, VEC> k[kBatch], v[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) k[u] = K.row(col[u]);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) v[u] = V.row(col[u]);
         if (w.e + n < w.end) w.fetch(a.p, w.e + n);
-        bool keep[O::N];
-        if (a.key.threshold) kept<G, false>(a.key, offset, w.i, col, h, t, a.bundle_log, keep);
-        int use[O::N];
-        bool masked = false;
+        int keep[O::N];
+        if (a.key.threshold) kept<G, false, R>(a.key, offset, w.i, col, h, t, a.bundle_log, keep);
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) {
-            const bool there = O::entry(t, o) < n, open = b[o] != -INFINITY;
-            use[o] = there && open ? -1 : 0;
-            masked = masked || (there && !open);
-        }
-        if (bias && __any(masked)) {
-#define SENSEI_WIPE(U) k[U].mask(O::template get<U>(use));
-            SENSEI_EACH(SENSEI_WIPE)
-#undef SENSEI_WIPE
-        }
-        float s[kBatch], c[kBatch], x[O::N], dv[O::N];
+        for (int r = 0; r < R; ++r) {
+            Q.keep_own(q[r]);
+            dY.keep_own(dy[r]);
+            int use[O::N];
+            bool masked = false;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            s[u] = dot(q, k[u]);
-            c[u] = dot(dy, v[u]);
-        }
-        O::sums(s, t, x);
-        O::sums(c, t, dv);
-        float pb[O::N];
+            for (int o = 0; o < O::N; ++o) {
+                const bool there = O::entry(t, o) < n, open = b[r][o] != -INFINITY;
+                use[o] = there && open ? -1 : 0;
+                masked = masked || (there && !open);
+            }
+            float s[kBatch], c[kBatch], x[O::N], dv[O::N], pb[O::N];
 #pragma unroll
-        for (int o = 0; o < O::N; ++o) {
-            const Score sc = score_of(a, x[o]);
-            const float dp = a.key.threshold && !keep[o] ? 0.f : dv[o] * a.key.keep_scale;
-            const float p = use[o] ? exp_neg((sc.x + b[o] - st.x) - st.y) : 0.f, dt = use[o] ? p * (dp - st.z) : 0.f, by = sc.slope * a.scale;
-            delta += dt;
-            x[o] = dt * by;
-            pb[o] = p * by;
-        }
-#define SENSEI_ADD(U)                                                 \
-    acc.add(O::template get<U>(x), k[U]);                             \
-    if constexpr (!WHOLE_Y) share.add(O::template get<U>(pb), k[U]);
-        SENSEI_EACH(SENSEI_ADD)
+            for (int u = 0; u < kBatch; ++u) {
+                s[u] = dot(q[r], k[u]);
+                c[u] = dot(dy[r], v[u]);
+            }
+            O::sums(s, t, x);
+            O::sums(c, t, dv);
+#pragma unroll
+            for (int o = 0; o < O::N; ++o) {
+                const Score sc = score_of(a, x[o]);
+                const float dp = a.key.threshold && !(keep[o] >> r & 1) ? 0.f : dv[o] * a.key.keep_scale;
+                const float p = use[o] ? exp_neg((sc.x + b[r][o] - st[r].x) - st[r].y) : 0.f, dt = use[o] ? p * (dp - st[r].z) : 0.f, by = sc.slope * a.scale;
+                delta[r] += dt;
+                x[o] = dt * by;
+                pb[o] = use[o] ? p * by : 0.f;
+                x[o] = use[o] ? x[o] : 0.f;
+            }
+            if (bias && __any(masked)) {
+#define SENSEI_ADD(U)                                                                                        \
+    acc[r].add(O::template get<U>(x), k[U], O::template get<U>(use));                                        \
+    if constexpr (!WHOLE_Y) share[r].add(O::template get<U>(pb), k[U], O::template get<U>(use));
+                SENSEI_EACH(SENSEI_ADD)
 #undef SENSEI_ADD
+            } else {
+#define SENSEI_ADD(U)                                                     \
+    acc[r].add(O::template get<U>(x), k[U]);                              \
+    if constexpr (!WHOLE_Y) share[r].add(O::template get<U>(pb), k[U]);
+                SENSEI_EACH(SENSEI_ADD)
+#undef SENSEI_ADD
+            }
+        }
         w.e += n;
         if (w.row_done()) {
-            const float off = WHOLE_Y ? 0.f : O::sum(delta);
-            if (at.head_live) {
-                if (!w.goes_on && w.e == w.row_end) {
-                    if (!WHOLE_Y) {
-                        acc.add(-off, share);
-                        if (t == 0) a.row_stats[(size_t)w.i * a.heads + h].z = st.z + off;
-                    }
-                    acc.store(dQ + (long long)w.i * a.ldo1, t, a.d, 1.f);
-                } else {
-                    const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h);
-                    float *to = a.piece + at_piece * ((WHOLE_Y ? 1 : 2) * G * VEC);
-                    acc.put(to, t);
-                    if (!WHOLE_Y) {
-                        share.put(to + G * VEC, t);
-                        if (t == 0) a.piece_ml[at_piece] = make_float2(off, 0.f);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float off = WHOLE_Y ? 0.f : O::sum(delta[r]);
+                if (at.head_live) {
+                    if (!w.goes_on && w.e == w.row_end) {
+                        if (!WHOLE_Y) {
+                            acc[r].add(-off, share[r]);
+                            if (t == 0) a.row_stats[(size_t)w.i * a.heads + h + r].z = st[r].z + off;
+                        }
+                        acc[r].store(dQ + (long long)w.i * a.ldo1 + r * a.d, t, a.d, 1.f);
+                    } else {
+                        const size_t at_piece = piece_at(at.chunk, w.goes_on, a.heads, h + r);
+                        float *to = a.piece + at_piece * ((WHOLE_Y ? 1 : 2) * G * VEC);
+                        acc[r].put(to, t);
+                        if (!WHOLE_Y) {
+                            share[r].put(to + G * VEC, t);
+                            if (t == 0) a.piece_ml[at_piece] = make_float2(off, 0.f);
+                        }
                     }
                 }
+                acc[r].zero();
+                if (!WHOLE_Y) share[r].zero();
+                delta[r] = 0.f;
             }
-            if (w.e < w.end) {
-                w.next_row(a.p);
-                acc.zero();
-                if (!WHOLE_Y) share.zero();
-                delta = 0.f;
-            }
+            if (w.e < w.end) w.next_row(a.p);
+            fresh = true;
         }
     }
 }
@@ -695,9 +757,11 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
         const int call_log = a.ratio == 1 ? a.bundle_log : 0;   // heads of one generator call lie side by side
         Walk w;
         w.begin(a.p, at.chunk, at.in_group, at.group_lanes);
+        Gathered<T, VEC> k, v;
         Sums<T, VEC, G, GENERIC> dk, dv;
         dk.zero();
         dv.zero();
+        bool fresh = true;
         while (w.e < w.end) {
             const int n = w.count();
             int row[kBatch], own[O::N], bin[O::N];
@@ -707,7 +771,11 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
                 own[o] = O::of(t, o, row);
                 bin[o] = bias ? w.bucket_of(O::entry(t, o), a.n_buckets) : 0;
             }
-            const Gathered<T, VEC> k = K.own(w.i), v = V.own(w.i);
+            if (fresh) {
+                k = K.row(w.i);
+                v = V.row(w.i);
+                fresh = false;
+            }
             for (int r = 0; r < a.ratio; ++r) {
                 const int h = g * a.ratio + r;
                 float b[O::N];
@@ -723,8 +791,10 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) dy[u] = dY.row(row[u], (long long)r * a.dv * (int)sizeof(T));
                 if (r == 0 && w.e + n < w.end) w.fetch(a.p, w.e + n);
-                bool keep[O::N];
-                if (a.key.threshold) kept<G, true>(a.key, offset, w.i, row, h, t, call_log, keep);
+                K.keep_own(k);
+                V.keep_own(v);
+                int keep[O::N];
+                if (a.key.threshold) kept<G, true, 1>(a.key, offset, w.i, row, h, t, call_log, keep);
                 int use[O::N];
                 bool masked = false;
 #pragma unroll
@@ -751,7 +821,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
 #pragma unroll
                 for (int o = 0; o < O::N; ++o) {
                     const Score sc = score_of(a, x[o]);
-                    const float ks = a.key.threshold && !keep[o] ? 0.f : a.key.keep_scale, dp = ks == 0.f ? 0.f : pw[o] * ks;
+                    const float ks = a.key.threshold && !(keep[o] & 1) ? 0.f : a.key.keep_scale, dp = ks == 0.f ? 0.f : pw[o] * ks;
                     const float p = use[o] ? exp_neg((sc.x + b[o] - st[o].x) - st[o].y) : 0.f, dt = use[o] ? p * (dp - st[o].z) : 0.f;
                     x[o] = dt * sc.slope * a.scale;
                     pw[o] = p * ks;
@@ -779,11 +849,10 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
                         dv.put(to + G * VEC, t);
                     }
                 }
-                if (w.e < w.end) {
-                    w.next_row(a.p);
-                    dk.zero();
-                    dv.zero();
-                }
+                dk.zero();
+                dv.zero();
+                if (w.e < w.end) w.next_row(a.p);
+                fresh = true;
             }
         }
     }
@@ -805,8 +874,17 @@ __global__ __launch_bounds__(1024) void k_attention_bias(const float *__restrict
     __shared__ double lds[64][16];
     const int k = blockIdx.x * 16 + (threadIdx.x & 15), seg = threadIdx.x >> 4;
     double s = 0.0;
-    if (k < n)
-        for (int b = seg; b < blocks; b += 64) s += (double)part[(size_t)b * n + k];
+    if (k < n) {
+        int b = seg;
+        for (; b + 7 * 64 < blocks; b += 8 * 64) {   // eight loads under way: one after the other they took 40 us of 5,700 blocks
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = part[(size_t)(b + u * 64) * n + k];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += (double)x[u];
+        }
+        for (; b < blocks; b += 64) s += (double)part[(size_t)b * n + k];
+    }
     lds[seg][threadIdx.x & 15] = s;
     for (int half = 32; half > 0; half >>= 1) {
         __syncthreads();
@@ -819,7 +897,7 @@ __global__ __launch_bounds__(1024) void k_attention_bias(const float *__restrict
 
 enum { kJoinForward = 0, kJoinRows = 1, kJoinCols = 2 };
 
-// A group per chunk boundary (and bundle of heads): where a row crosses it that crossed none before, the group joins that row's pieces, in their order; a
+// A group of lanes per chunk boundary and bundle of heads (blockIdx.y): where a row crosses it that crossed none before, the group joins that row's pieces, in their order; a
 // row of more than kManyPieces is left to the whole wavefront, whose groups take them in turn.  Workgroups behind those (of the first bundle)
 // look over 64 rows a wavefront and write the rows without entries.
 constexpr int kManyPieces = 16;
@@ -842,7 +920,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
         }
         return;
     }
-    const int groups = (64 / G) >> a.bundle_log, t = lane % G, slot = lane / G, group = slot >> a.bundle_log;
+    const int groups = (64 / G) >> a.bundle_log, group_lanes = G << a.bundle_log, t = lane % G, slot = lane / G, group = slot >> a.bundle_log;
     const int head = ((int)blockIdx.y << a.bundle_log) + (slot & ((1 << a.bundle_log) - 1)), h = head < n_heads ? head : n_heads - 1;
     // the first piece's chunk and the number of pieces of the row that first crosses the group's boundary; 0: there is none
     int first = wave * groups + group, pieces = 0, i = 0;
@@ -901,7 +979,6 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
         for (int k = 0; k < pieces; ++k) take(first, k);
         finish(i);
     }
-    const int group_lanes = G << a.bundle_log;
     for (int o = 0; o < groups; ++o) {
         if (!(many >> (o * group_lanes) & 1)) continue;     // the same for the whole wavefront
         const int from = __shfl(first, o * group_lanes, 64), row = __shfl(i, o * group_lanes, 64), n = __shfl(pieces, o * group_lanes, 64);
@@ -953,12 +1030,13 @@ __global__ __launch_bounds__(kThreads) void k_attention_row_stats(AttnArgs a, un
 
 // ------------------------------------------------------------------------------------------------------------------ host side
 
-// Lanes of a head, from the wider of a head's key and value: 32 bytes a lane.  Tables of dbias (`table` floats a head) are kept for every head that a
+// Lanes of a head, from the wider of a head's key and value: 32 bytes a lane; 8 elements where a lane takes several query heads (16 of them and
+// their sums would leave a SIMD one wavefront).  Tables of dbias (`table` floats a head) are kept for every head that a
 // wavefront works on: more lanes a head where those would not fit 64 KB.
 struct Shape { int vec, lanes; };
-Shape shape_of(int d, int dv, int elem, int table) {
+Shape shape_of(int d, int dv, int elem, int heads_a_lane, int table) {
     const int w = d > dv ? d : dv;
-    Shape s{32 / elem, 1};
+    Shape s{heads_a_lane > 1 ? 8 : 32 / elem, 1};
     while (s.lanes * s.vec < w || (size_t)(64 / s.lanes) * table * sizeof(float) > 65536) s.lanes *= 2;
     return s;
 }
@@ -976,20 +1054,50 @@ int chunk_of(int64_t nnz, int bundles, int groups) {
     return t;
 }
 
+// Gathers by 24-bit products and 32-bit offsets, whole pieces: every number of a row and of bytes a row below 2^24, every matrix below 4 GB, heads
+// no narrower than a piece.
+bool plain_gathers(const AttentionCall &c) {
+    const int per = 16 / c.elem;
+    if (c.d < per || c.dv < per || c.A->n_rows >= 1 << 24 || c.A->n_cols >= 1 << 24) return false;
+    struct { int64_t rows, ld; } m[] = {{c.A->n_cols, c.ldk}, {c.A->n_cols, c.ldv}, {c.A->n_rows, c.ldq}, {c.At ? c.A->n_rows : 0, c.lddy}, {c.At ? c.A->n_rows : 0, c.ldy}};
+    for (const auto &x : m)
+        if (x.rows && (x.ld * c.elem >= 1 << 24 || x.rows * x.ld * c.elem > 0xFFFFFFFFll)) return false;
+    return true;
+}
+
+enum Walks { kForward, kRows, kCols };
 struct Layout {
     Shape shape;
+    int heads_a_lane;                              // R of the walk
     int bundle_log, bundles, groups, chunk, n_chunks;
-    Layout(const AttentionCall &c, bool cols) {
+    int join_log, join_bundles;                    // bundles of the pass that joins the pieces: eight lanes, 256 bytes of the pieces and more
+    // A lane takes two query heads of a key head together where heads are wider than 128 bytes: what they gather is the same, and a wavefront has twice as
+    // much of different rows under way.  One / two / four heads a lane, us: forward, fp32, 184,000 rows of 15, 16 heads of 96 on 4 2,780 / 2,158 / 2,279;
+    // 212,000 nodes of 22, 6 heads of 128 on 3 1,770 / 1,482; training, fp16, 51,000 rows of 60, 4 heads of 96 on 1 1,951 / 1,757 / 1,812.  Narrower heads
+    // lose the lanes that would share out their entries: bf16, 233,000 nodes of 87, 8 heads of 64 on 2 1,978 / 2,057 / 2,371.
+    static int together_of(const AttentionCall &c, Walks walk, bool plain) {
+        return walk != kCols && plain && c.heads / c.kv_heads % 2 == 0 && (c.d > c.dv ? c.d : c.dv) * c.elem > 128 ? 2 : 1;
+    }
+    Layout(const AttentionCall &c, Walks walk, bool plain) {
         const int64_t nnz = c.A->nnz;
-        const int n_heads = cols ? c.kv_heads : c.heads, together = cols ? 1 : c.heads / c.kv_heads, elem = c.elem, d = c.d, dv = c.dv;
-        shape = shape_of(d, dv, elem, c.dbias ? c.heads / c.kv_heads * c.n_buckets : 0);
+        heads_a_lane = together_of(c, walk, plain);
+        const bool cols = walk == kCols;
+        const int all = cols ? c.kv_heads : c.heads, n_heads = all / heads_a_lane, together = cols ? 1 : c.heads / c.kv_heads / heads_a_lane, elem = c.elem, d = c.d, dv = c.dv;
+        shape = shape_of(d, dv, elem, heads_a_lane, cols && c.dbias ? c.heads / c.kv_heads * c.n_buckets : 0);
         bundle_log = bundle_log_of(shape, n_heads, together, (d > dv ? d : dv) * elem);
         bundles = (n_heads + (1 << bundle_log) - 1) >> bundle_log;
         groups = (64 / shape.lanes) >> bundle_log;
         chunk = chunk_of(nnz, bundles, groups);
         n_chunks = (int)((nnz + chunk - 1) / chunk);
+        join_log = 0;
+        while ((shape.lanes << join_log) < 8 && (1 << join_log) < all) ++join_log;
+        join_bundles = (all + (1 << join_log) - 1) >> join_log;
     }
     int blocks(int waves) const { return (n_chunks + waves * groups - 1) / (waves * groups); }
+    int join_blocks(int waves) const {
+        const int per = waves * ((64 / shape.lanes) >> join_log);
+        return n_chunks > 1 ? (n_chunks + per - 1) / per : 0;
+    }
     size_t rows_bytes() const { return align_up((size_t)n_chunks * sizeof(int32_t), 256); }
     size_t piece_bytes(int n_heads, int sums) const { return align_up((size_t)n_chunks * 2 * n_heads * shape.vec * shape.lanes * sums * sizeof(float), 256); }
     size_t ml_bytes(int n_heads) const { return align_up((size_t)n_chunks * 2 * n_heads * sizeof(float2), 256); }
@@ -1005,8 +1113,7 @@ struct Room {   // what the backward carves its scratch into
     Layout rows, cols;
     int col_waves;
     size_t bucket, stats, piece, ml, bias;
-    Room(const AttentionCall &c)
-        : rows(c, false), cols(c, true) {
+    Room(const AttentionCall &c, bool plain) : rows(c, kRows, plain), cols(c, kCols, plain) {
         col_waves = table_waves(c, cols.shape);
         bucket = c.n_buckets > 0 ? align_up((size_t)c.A->nnz, 256) : 0;
         stats = align_up((size_t)c.A->n_rows * c.heads * sizeof(float4), 256);
@@ -1017,17 +1124,6 @@ struct Room {   // what the backward carves its scratch into
     }
     size_t bytes() const { return rows.rows_bytes() + cols.rows_bytes() + bucket + stats + piece + ml + bias; }
 };
-
-// Gathers by 24-bit products and 32-bit offsets, whole pieces: every number of a row and of bytes a row below 2^24, every matrix below 4 GB, heads
-// no narrower than a piece.
-bool plain_gathers(const AttentionCall &c, const Shape &s) {
-    const int per = 16 / c.elem;
-    if (c.d < per || c.dv < per || c.A->n_rows >= 1 << 24 || c.A->n_cols >= 1 << 24) return false;
-    struct { int64_t rows, ld; } m[] = {{c.A->n_cols, c.ldk}, {c.A->n_cols, c.ldv}, {c.At ? c.A->n_rows : 0, c.ldq}, {c.At ? c.A->n_rows : 0, c.lddy}};
-    for (const auto &x : m)
-        if (x.rows && (x.ld * c.elem >= 1 << 24 || x.rows * x.ld * c.elem > 0xFFFFFFFFll)) return false;
-    return true;
-}
 
 AttnArgs args_of(const AttentionCall &c) {
     AttnArgs a = {};
@@ -1046,62 +1142,93 @@ WalkPattern pattern_of(const sensei_csr &A, const Layout &l, const uint8_t *buck
     return {A.row_ptr, A.col_idx, bucket, chunk_row, A.n_rows, (int)A.nnz, l.chunk, l.n_chunks};
 }
 
-template <class T, int VEC, int G, bool GENERIC, int MODE> hipError_t join_and_fill(const AttnArgs &a, const Layout &l, int n_heads, hipStream_t s) {
+template <class T, int VEC, int G, bool GENERIC, int MODE> hipError_t join_and_fill(AttnArgs a, const Layout &l, int n_heads, hipStream_t s) {
     constexpr int waves = kThreads / 64;
-    const int join_blocks = l.n_chunks > 1 ? l.blocks(waves) : 0, fill = (int)((a.p.n_rows + 64ll * waves - 1) / (64 * waves));
+    a.bundle_log = l.join_log;
+    const int join_blocks = l.join_blocks(waves), fill = (int)((a.p.n_rows + 64ll * waves - 1) / (64 * waves));
     if (join_blocks + fill == 0) return hipSuccess;
-    hipLaunchKernelGGL((k_attention_join<T, VEC, G, MODE, GENERIC>), dim3(join_blocks + fill, l.bundles), dim3(kThreads), 0, s, a, n_heads, join_blocks);
+    hipLaunchKernelGGL((k_attention_join<T, VEC, G, MODE, GENERIC>), dim3(join_blocks + fill, l.join_bundles), dim3(kThreads), 0, s, a, n_heads, join_blocks);
     return hipGetLastError();
 }
 
-template <class T, int VEC, int G, bool GENERIC> hipError_t forward_shape(AttnArgs a, const Layout &l, hipStream_t s) {
-    if (a.p.nnz > 0) hipLaunchKernelGGL((k_attention<T, VEC, G, GENERIC>), dim3(l.blocks(kThreads / 64), l.bundles), dim3(kThreads), 0, s, a);
+// VEC elements a lane: 8 of fp32 whatever R, of 16 bits 16 with R = 1 and 8 with others
+template <class T, int VEC, int R> constexpr bool kShaped = sizeof(T) == 4 || (R == 1) == (VEC == 16);
+
+template <class T, int VEC, int G, bool GENERIC> hipError_t forward_shape(const AttnArgs &a, const Layout &l, hipStream_t s) {
+    const dim3 grid(l.blocks(kThreads / 64), l.bundles), block(kThreads);
+    if (a.p.nnz > 0) {
+        if constexpr (!GENERIC && kShaped<T, VEC, 2>) {
+            if (l.heads_a_lane == 2) hipLaunchKernelGGL((k_attention<T, VEC, G, GENERIC, 2>), grid, block, 0, s, a);
+        }
+        if constexpr (kShaped<T, VEC, 1>) {
+            if (l.heads_a_lane == 1) hipLaunchKernelGGL((k_attention<T, VEC, G, GENERIC, 1>), grid, block, 0, s, a);
+        }
+    }
     return join_and_fill<T, VEC, G, GENERIC, kJoinForward>(a, l, a.heads, s);
 }
 
-template <class T, int VEC, int G, bool GENERIC> hipError_t backward_shape(const AttentionCall &c, AttnArgs a, const Room &room, const WalkPattern &pr, const WalkPattern &pc,
-                                                                           hipStream_t s) {
-    hipError_t e;
-    a.p = pr;
+// (m, log l, D) and dQ
+template <class T, int VEC, int G, bool GENERIC> hipError_t rows_shape(const AttentionCall &c, AttnArgs a, const Layout &l, uint8_t *bucket_t, hipStream_t s) {
     a.O1 = c.dQ; a.ldo1 = c.lddq;
-    a.bundle_log = room.rows.bundle_log;
-    if (pr.nnz > 0) {
-        const unsigned blocks = (unsigned)(((int64_t)pr.n_rows * a.heads + kThreads / G - 1) / (kThreads / G)), more = a.bias ? (unsigned)((pr.nnz + kThreads - 1) / kThreads) : 0;
-        hipLaunchKernelGGL((k_attention_row_stats<T, VEC, G, GENERIC>), dim3(blocks + more), dim3(kThreads), 0, s, a, blocks, c.bucket, c.t_pos, pr.nnz, const_cast<uint8_t *>(pc.bucket));
-        hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G, GENERIC>), dim3(room.rows.blocks(kThreads / 64), room.rows.bundles), dim3(kThreads), 0, s, a);
+    a.bundle_log = l.bundle_log;
+    if (a.p.nnz > 0) {
+        const unsigned blocks = (unsigned)(((int64_t)a.p.n_rows * a.heads + kThreads / G - 1) / (kThreads / G)), more = a.bias ? (unsigned)((a.p.nnz + kThreads - 1) / kThreads) : 0;
+        hipLaunchKernelGGL((k_attention_row_stats<T, VEC, G, GENERIC>), dim3(blocks + more), dim3(kThreads), 0, s, a, blocks, c.bucket, c.t_pos, a.p.nnz, bucket_t);
+        const dim3 grid(l.blocks(kThreads / 64), l.bundles), block(kThreads);
+        if constexpr (!GENERIC && kShaped<T, VEC, 2>) {
+            if (l.heads_a_lane == 2) hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G, GENERIC, 2>), grid, block, 0, s, a);
+        }
+        if constexpr (kShaped<T, VEC, 1>) {
+            if (l.heads_a_lane == 1) hipLaunchKernelGGL((k_attention_back_rows<T, VEC, G, GENERIC, 1>), grid, block, 0, s, a);
+        }
     }
-    if ((e = join_and_fill<T, VEC, G, GENERIC, kJoinRows>(a, room.rows, a.heads, s)) != hipSuccess) return e;
-    a.p = pc;
-    a.O1 = c.dK; a.ldo1 = c.lddk;
-    a.O2 = c.dV; a.ldo2 = c.lddv;
-    a.bundle_log = room.cols.bundle_log;
-    if (pc.nnz > 0) {
-        const int blocks = room.cols.blocks(room.col_waves), n = a.heads * a.n_buckets;
-        const size_t lds = a.bias_part ? (size_t)room.col_waves * (64 / G) * a.ratio * a.n_buckets * sizeof(float) : 0;
-        hipLaunchKernelGGL((k_attention_back_cols<T, VEC, G, GENERIC>), dim3(blocks, room.cols.bundles), dim3(64 * room.col_waves), lds, s, a);
-        if (a.bias_part) hipLaunchKernelGGL(k_attention_bias, dim3((n + 15) / 16), dim3(1024), 0, s, a.bias_part, blocks, n, c.dbias);
+    return join_and_fill<T, VEC, G, GENERIC, kJoinRows>(a, l, a.heads, s);
+}
+
+// dK, dV and dbias
+template <class T, int VEC, int G, bool GENERIC> hipError_t cols_shape(const AttentionCall &c, AttnArgs a, const Room &room, hipStream_t s) {
+    if constexpr (kShaped<T, VEC, 1>) {
+        const Layout &l = room.cols;
+        a.O1 = c.dK; a.ldo1 = c.lddk;
+        a.O2 = c.dV; a.ldo2 = c.lddv;
+        a.bundle_log = l.bundle_log;
+        if (a.p.nnz > 0) {
+            const int blocks = l.blocks(room.col_waves), n = a.heads * a.n_buckets;
+            const size_t lds = a.bias_part ? (size_t)room.col_waves * (64 / G) * a.ratio * a.n_buckets * sizeof(float) : 0;
+            hipLaunchKernelGGL((k_attention_back_cols<T, VEC, G, GENERIC>), dim3(blocks, l.bundles), dim3(64 * room.col_waves), lds, s, a);
+            if (a.bias_part) hipLaunchKernelGGL(k_attention_bias, dim3((n + 15) / 16), dim3(1024), 0, s, a.bias_part, blocks, n, c.dbias);
+        }
+        return join_and_fill<T, VEC, G, GENERIC, kJoinCols>(a, l, a.kv_heads, s);
     }
-    return join_and_fill<T, VEC, G, GENERIC, kJoinCols>(a, room.cols, a.kv_heads, s);
+    return hipErrorInvalidValue;   // no layout has this shape
 }
 
 #define SENSEI_BY_SHAPE(T, VEC, lanes, GEN, CALL)                                                              \
     (lanes == 1 ? CALL(T, VEC, 1, GEN) : lanes == 2 ? CALL(T, VEC, 2, GEN) : lanes == 4 ? CALL(T, VEC, 4, GEN) \
      : lanes == 8 ? CALL(T, VEC, 8, GEN) : lanes == 16 ? CALL(T, VEC, 16, GEN) : CALL(T, VEC, 32, GEN))
 #define SENSEI_BY_GATHER(T, VEC, lanes, plain, CALL) (plain ? SENSEI_BY_SHAPE(T, VEC, lanes, false, CALL) : SENSEI_BY_SHAPE(T, VEC, lanes, true, CALL))
-#define SENSEI_BY_TYPE(type, lanes, plain, CALL)                                                                             \
-    (type == SENSEI_F32 ? SENSEI_BY_GATHER(float, 8, lanes, plain, CALL) : type == SENSEI_BF16 ? SENSEI_BY_GATHER(Bf16, 16, lanes, plain, CALL) \
-     : SENSEI_BY_GATHER(F16, 16, lanes, plain, CALL))
+#define SENSEI_BY_VEC(T, vec, lanes, plain, CALL) (vec == 16 ? SENSEI_BY_GATHER(T, 16, lanes, plain, CALL) : SENSEI_BY_SHAPE(T, 8, lanes, false, CALL))
+#define SENSEI_BY_TYPE(type, shape, plain, CALL)                                                                                                   \
+    (type == SENSEI_F32 ? SENSEI_BY_GATHER(float, 8, shape.lanes, plain, CALL) : type == SENSEI_BF16 ? SENSEI_BY_VEC(Bf16, shape.vec, shape.lanes, plain, CALL) \
+     : SENSEI_BY_VEC(F16, shape.vec, shape.lanes, plain, CALL))
 
 }  // namespace
 
+// The queries do not know the leading dimensions: room for either kind of gathers.
 size_t attention_ws_bytes(const AttentionCall &c) {
-    const Layout l(c, false);
-    return l.rows_bytes() + l.piece_bytes(c.heads, 1) + l.ml_bytes(c.heads) + 256;
+    size_t most = 0;
+    for (const bool plain : {false, true}) {
+        const Layout l(c, kForward, plain);
+        const size_t n = l.rows_bytes() + l.piece_bytes(c.heads, 1) + l.ml_bytes(c.heads) + 256;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s) {
     if (c.A->n_rows <= 0) return hipSuccess;
-    const Layout l(c, false);
+    const bool plain = plain_gathers(c);
+    const Layout l(c, kForward, plain);
     AttnArgs a = args_of(c);
     int32_t *chunk_row = reinterpret_cast<int32_t *>(ws);
     a.p = pattern_of(*c.A, l, a.bias ? c.bucket : nullptr, chunk_row);
@@ -1109,16 +1236,19 @@ hipError_t launch_attention(const AttentionCall &c, char *ws, hipStream_t s) {
     a.piece_ml = reinterpret_cast<float2 *>(ws + l.rows_bytes() + l.piece_bytes(c.heads, 1));
     a.O1 = c.out; a.ldo1 = c.ldo;
     a.bundle_log = l.bundle_log;
-    const bool plain = plain_gathers(c, l.shape);
 #define SENSEI_CALL(T, V, G, GEN) forward_shape<T, V, G, GEN>(a, l, s)
-    return SENSEI_BY_TYPE(c.type, l.shape.lanes, plain, SENSEI_CALL);
+    return SENSEI_BY_TYPE(c.type, l.shape, plain, SENSEI_CALL);
 #undef SENSEI_CALL
 }
 
-size_t attention_backward_ws_bytes(const AttentionCall &c) { return Room(c).bytes() + 256; }
+size_t attention_backward_ws_bytes(const AttentionCall &c) {
+    const size_t a = Room(c, false).bytes(), b = Room(c, true).bytes();
+    return (a > b ? a : b) + 256;
+}
 
 hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream_t s) {
-    const Room room(c);
+    const bool plain = plain_gathers(c);
+    const Room room(c, plain);
     AttnArgs a = args_of(c);
     char *at = ws;
     auto take = [&](size_t n) { char *p = at; at += n; return p; };
@@ -1128,14 +1258,18 @@ hipError_t launch_attention_backward(const AttentionCall &c, char *ws, hipStream
     a.piece = reinterpret_cast<float *>(take(room.piece));
     a.piece_ml = reinterpret_cast<float2 *>(take(room.ml));
     a.bias_part = a.bias && c.dbias ? reinterpret_cast<float *>(take(room.bias)) : nullptr;
-    const WalkPattern pr = pattern_of(*c.A, room.rows, a.bias ? c.bucket : nullptr, rows_r), pc = pattern_of(*c.At, room.cols, a.bias ? bucket_t : nullptr, rows_c);
     if (c.A->nnz == 0 && a.bias_part) {
         const hipError_t e = launch_zero_matrix(c.dbias, 1, c.heads * c.n_buckets, c.heads * c.n_buckets, false, s);
         if (e != hipSuccess) return e;
     }
-    const bool plain = plain_gathers(c, room.rows.shape);
-#define SENSEI_CALL(T, V, G, GEN) backward_shape<T, V, G, GEN>(c, a, room, pr, pc, s)
-    return SENSEI_BY_TYPE(c.type, room.rows.shape.lanes, plain, SENSEI_CALL);
+    a.p = pattern_of(*c.A, room.rows, a.bias ? c.bucket : nullptr, rows_r);
+#define SENSEI_CALL(T, V, G, GEN) rows_shape<T, V, G, GEN>(c, a, room.rows, bucket_t, s)
+    const hipError_t e = SENSEI_BY_TYPE(c.type, room.rows.shape, plain, SENSEI_CALL);
+#undef SENSEI_CALL
+    if (e != hipSuccess) return e;
+    a.p = pattern_of(*c.At, room.cols, a.bias ? bucket_t : nullptr, rows_c);
+#define SENSEI_CALL(T, V, G, GEN) cols_shape<T, V, G, GEN>(c, a, room, s)
+    return SENSEI_BY_TYPE(c.type, room.cols.shape, plain, SENSEI_CALL);
 #undef SENSEI_CALL
 }
 
