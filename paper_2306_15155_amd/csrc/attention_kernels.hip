@@ -1048,10 +1048,14 @@ int bundle_log_of(const Shape &s, int n_heads, int together, int bytes) {
     while ((s.lanes << (log + 1)) <= 64 && (1 << log) < n_heads && ((bytes << log) / together < 256 || (1 << log) < together)) ++log;
     return log;
 }
+// Entries of a chunk: as many as leave 16,384 wavefronts, 32 to 256, so that chunks of many short rows (a batch each, however few their entries) even out;
+// 16 where a SIMD would have less than a wavefront.  4,096 / 8,192 / 16,384 / 32,768 wavefronts, us: training steps, power-law patterns, 100,000 nodes
+// of 21 1,376 / 1,103 / 1,044 / 1,036, 212,000 of 22 1,662 / 1,676 / 1,452 / 1,449 (forward); batched graphs of 290,000 nodes 2,354 / 2,155 / 2,265 /
+// 2,666; 123,000 rows of 48 288 / 300 / 337 / 410 (forward).  Chunks of 16 / 32 entries: 10,000 nodes of 11 21 / 26.
 int chunk_of(int64_t nnz, int bundles, int groups) {
     int t = 256;
     while (t > 32 && nnz / t * bundles / groups < 16384) t >>= 1;
-    return t;
+    return t == 32 && nnz / t * bundles / groups < 1024 ? 16 : t;
 }
 
 // Gathers by 24-bit products and 32-bit offsets, whole pieces: every number of a row and of bytes a row below 2^24, every matrix below 4 GB, heads
