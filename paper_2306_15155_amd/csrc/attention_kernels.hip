@@ -54,21 +54,6 @@ struct AttnArgs {
 
 // ------------------------------------------------------------------------------------------------------------------ lanes of a head
 
-template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)); }
-template <int CTRL> __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
-
-__device__ __forceinline__ float from_16_away(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
-
-// sum over the G lanes of a head, in all of them (the lanes of a head are always active together)
-template <int G> __device__ __forceinline__ float head_sum(float x) {
-    if (G >= 2) x += dpp<0xB1>(x);           // the neighbour in a pair
-    if (G >= 4) x += dpp<0x4E>(x);           // the other pair of a quad
-    if (G >= 8) x += dpp<0x141>(x);          // mirrored within eight lanes
-    if (G >= 16) x += dpp<0x140>(x);         // mirrored within sixteen
-    if (G >= 32) x += from_16_away(x);
-    return x;
-}
-
 // What a head's lanes work out for the four entries of a batch: lane t has entry t % 4, with two lanes a head entries t and t + 2, a lone lane all.
 template <int G> struct Own {
     static constexpr int N = G >= 4 ? 1 : 4 / G, SHARERS = G < 4 ? G : 4;
@@ -127,7 +112,7 @@ template <int G> struct Own {
         if (G >= 4) x = fmaxf(x, dpp<0x4E>(x));
         return x;
     }
-    __device__ __forceinline__ static float sum(float x) { return head_sum<SHARERS>(x); }
+    __device__ __forceinline__ static float sum(float x) { return sum_over<SHARERS>(x); }
 };
 
 // The number as it is, but worked on here: what follows from it is not kept from outside a loop in registers that are short there.
@@ -1024,7 +1009,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_row_stats(AttnArgs a, un
     float d = 0.f;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) d = fmaf(dy.get(k), y.get(k), d);
-    d = head_sum<G>(d);
+    d = sum_over<G>(d);
     if (t == 0) a.row_stats[at] = make_float4(ml.x, ml.y, d, 0.f);
 }
 

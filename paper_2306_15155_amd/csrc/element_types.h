@@ -50,6 +50,25 @@ __device__ __forceinline__ float exp_neg(float x) {
     return x < -104.f ? 0.f : fmaf(e * kLn2, r, e);
 }
 
+// ---- moves between lanes
+template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)); }
+template <int CTRL> __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
+__device__ __forceinline__ float from_16_away(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)); }
+
+// x joined over L neighbouring lanes (1 to 64, all active) by an operation whose order does not matter but for rounding, in all of them: the
+// neighbour in a pair, the other pair of a quad, lanes mirrored within eight and within sixteen, the other sixteen, the other half
+template <int L, class Op> __device__ __forceinline__ float over_lanes(float x, Op op) {
+    if (L >= 2) x = op(x, dpp<0xB1>(x));
+    if (L >= 4) x = op(x, dpp<0x4E>(x));
+    if (L >= 8) x = op(x, dpp<0x141>(x));
+    if (L >= 16) x = op(x, dpp<0x140>(x));
+    if (L >= 32) x = op(x, from_16_away(x));
+    if (L >= 64) x = op(x, __shfl_xor(x, 32, 64));
+    return x;
+}
+template <int L> __device__ __forceinline__ float sum_over(float x) { return over_lanes<L>(x, [](float a, float b) { return a + b; }); }
+template <int L> __device__ __forceinline__ float max_over(float x) { return over_lanes<L>(x, [](float a, float b) { return fmaxf(a, b); }); }
+
 // ---- Philox4x32 with seven rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; 2011): four words of 32 bits from a
 // 128-bit counter and a 64-bit key, nothing kept between calls, so a mask is formed again wherever it is needed.  Seven rounds are the
 // fewest that the authors report to pass every test of BigCrush; ten, their default, would make the dropping of 16-bit elements bound by

@@ -104,35 +104,48 @@ template <class T, bool ADD> hipError_t dropout_units(DropArgs a, long long rows
 
 // -------------------------------------------------------------------------------------------------------- log probabilities of labels
 
-// One row of C logits z, in one pass: with a running maximum m,
-//     s = sum exp(z - m),  t = sum (z - m) exp(z - m);   lse = m + log s,  entropy = log s - t / s,  log p_j = z_j - lse,
-// m raised to m' multiplies s by f = exp(m - m') and turns t into (t + (m - m') s) f.  Classes at -inf have no share (and add 0 to t); a
-// row of nothing else has lse = -inf.
+// One row of C logits z: with its maximum m,
+//     s = sum exp(z - m),  t = sum (z - m) exp(z - m);   lse = m + log s,  entropy = log s - t / s,  log p_j = (z_j - m) - log s.
+// Classes at -inf have no share (and add 0 to t); a row of nothing else has lse = -inf.  The exponential of an element is one fused product and one
+// instruction: exp(z - m) = 2^(z L - c) 2^(c - m L), L = log2(e) in fp32, c = m L rounded: the second factor, the same for a whole row, is put right in
+// log s.  Where m L has no room in fp32 (rows of a type's lowest value) the difference is formed first.
+struct RowBase {
+    float m, c;      // c finite, or -inf: differences
+    bool direct;
+    __device__ __forceinline__ explicit RowBase(float top) {
+#pragma clang fp contract(off)   // c is the rounded product wherever it goes
+        m = top > -INFINITY ? top : 0.f;
+        direct = !(fabsf(m) < 1e30f);      // and an infinite maximum, whose row is NaN whatever is done
+        c = direct ? 0.f : m * kLog2E;
+    }
+    __device__ __forceinline__ float power(float z) const { return direct ? exp_neg(z - m) : __builtin_amdgcn_exp2f(fmaf(z, kLog2E, -c)); }
+    // log of a power over that of exp(z - m); log of a sum of powers as if they were exp(z - m)
+    __device__ __forceinline__ float shift() const { return direct ? 0.f : fmaf(m, kLog2E, -c) * kLn2; }
+    __device__ __forceinline__ float log_sum(float s) const { return logf(s) - shift(); }
+};
+
+// Sums of a part of a row whose maximum is known to be at least every element of it.
 struct RowSum {
-    float m, s, t;
+    float m, s, t;   // powers relative to m
     __device__ __forceinline__ static RowSum empty() { return {-INFINITY, 0.f, 0.f}; }
-    __device__ __forceinline__ void raise(float top) {   // top >= m, not both -inf
-        const float d = m - top;
+    __device__ __forceinline__ void raise(float top) {   // top > m
         if (m > -INFINITY) {
-            const float f = exp_neg(d);
-            t = f == 0.f ? 0.f : fmaf(d, s, t) * f;   // d may be as low as a type's lowest value
+            const RowBase old(m), now(top);
+            // powers of the old base to those of the new one
+            const float f = old.direct || now.direct ? exp_neg(m - top) : __builtin_amdgcn_exp2f(old.c - now.c);
+            t = f == 0.f ? 0.f : fmaf(m - top, s, t) * f;   // the difference may be as low as a type's lowest value
             s *= f;
         }
         m = top;
     }
     __device__ __forceinline__ void join(const RowSum &o) {
-        const float top = fmaxf(m, o.m);
-        if (top > -INFINITY) {
-            RowSum b = o;
-            raise(top);
-            b.raise(top);
-            s += b.s;
-            t += b.t;
-        } else {   // nothing but -inf and NaN so far
-            s += o.s;
-            t += o.t;
-        }
+        RowSum b = o;
+        if (b.m > m) raise(b.m);
+        else if (m > b.m) b.raise(m);
+        s += b.s;
+        t += b.t;
     }
+    __device__ __forceinline__ float log_sum() const { return RowBase(m).log_sum(s); }
     // z - lse, the large numbers first: exact where m is far from 0 (a row of nothing but a type's lowest value)
     __device__ __forceinline__ float log_p(float z, float log_s) const { return s == 0.f ? -INFINITY : (z - m) - log_s; }
 };
@@ -171,7 +184,7 @@ struct LogArgs {
     void *dZ;
     long long lddz;
 };
-constexpr int kLogThreads = 256;
+constexpr int kLogThreads = 256, kMaxParts = 64;
 
 // A lane's R highest classes among those it has seen, in order.
 template <int R> struct Highest {
@@ -192,6 +205,8 @@ template <int R> struct Highest {
         }
         if (k > key[0]) { key[0] = k; cls[0] = c; }
     }
+    // what a class has to be above to be seen: NaN (nothing is known to be below it) while the list has room
+    __device__ __forceinline__ float least() const { return key[R - 1] ? order_value(key[R - 1]) : NAN; }
     __device__ __forceinline__ Rank head() const { return key[0] ? rank_of(key[0], cls[0]) : 0; }
     __device__ __forceinline__ void pop() {
 #pragma unroll
@@ -212,11 +227,6 @@ template <int L> __device__ __forceinline__ Rank max_over_lanes(Rank r) {
     }
     return r;
 }
-template <int L> __device__ __forceinline__ RowSum join_lanes(RowSum v) {
-#pragma unroll
-    for (int d = (L < 64 ? L : 64) / 2; d > 0; d >>= 1) v.join({__shfl_xor(v.m, d, 64), __shfl_xor(v.s, d, 64), __shfl_xor(v.t, d, 64)});
-    return v;
-}
 
 template <class T> __device__ __forceinline__ void finish_row(const LogArgs &a, long long row, const RowSum &v, float log_s, const T *z) {
     if (a.stats) a.stats[row] = make_float2(v.m, log_s);
@@ -227,120 +237,215 @@ template <class T> __device__ __forceinline__ void finish_row(const LogArgs &a, 
     }
 }
 
-// L lanes a row (4, 16, 64, or a workgroup's 256), 16 bytes a lane and step.  R: classes a lane keeps for the alternatives (0: none asked for); the
-// alternatives are then drawn one after the other, each the highest head of all lanes' lists.  A lane whose list was drawn empty goes over its
-// classes again for those behind the last one drawn: rare (more than R of a row's highest in one lane) and exact.
-template <class T, int L, int R>
-__global__ __launch_bounds__(kLogThreads) void k_logprobs(LogArgs a) {
-    constexpr int E = kPerPiece<T>, U = 4;
-    __shared__ RowSum wave_sum[4];
-    __shared__ Rank wave_top[2][4];
-    const int lane = threadIdx.x % L, wave = threadIdx.x / 64;
-    const long long unit = (long long)blockIdx.x * (kLogThreads / L) + threadIdx.x / L;
-    const long long row = a.row0 + (L == 256 ? unit / a.parts : unit);
-    const int part = L == 256 ? (int)(unit % a.parts) : 0;
-    const bool live = row < a.rows;      // whole groups of lanes; nobody leaves before the workgroup's exchanges
-    const T *z = static_cast<const T *>(a.Z) + (live ? row : 0) * a.ld;
-    const int c0 = L == 256 ? part * a.part_classes : 0;
-    const int c1 = !live ? c0 : L == 256 && c0 + a.part_classes < a.classes ? c0 + a.part_classes : a.classes;
-    RowSum v = RowSum::empty();
-    Highest<R> best;
-    best.clear();
-    auto take = [&](const T *x, int c, int n) {   // n classes from c on, n <= E
-        float f[E], top = -INFINITY;
+// E classes side by side into the sums (relative to base, which is at least their maximum)
+template <class T, int E> __device__ __forceinline__ void add_powers(RowSum &v, const RowBase &base, const float (&f)[E]) {
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-            f[k] = k < n ? to_f32(x[k]) : -INFINITY;
-            top = fmaxf(top, f[k]);
-        }
-        if (top > v.m) v.raise(top);
-        const float base = v.m > -INFINITY ? v.m : 0.f;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const float d = f[k] - base, e = exp_neg(d);
-            v.s += e;
-            v.t = fmaf(e, fmaxf(d, -FLT_MAX), v.t);
-        }
-        if (R > 0) {
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-                if (k < n) best.see(order_key(f[k]), c + k);
-        }
-    };
-    int c = c0 + lane * E;
-    for (; c + (U - 1) * L * E + E <= c1; c += U * L * E) {
-        Piece<T, E> x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = Piece<T, E>::load(z + c + u * L * E);
-#pragma unroll
-        for (int u = 0; u < U; ++u) take(x[u].x, c + u * L * E, E);
+    for (int k = 0; k < E; ++k) {
+        const float e = base.power(f[k]);
+        v.s += e;
+        v.t = fmaf(e, fmaxf(f[k] - base.m, -FLT_MAX), v.t);   // -inf: 0 times a finite number
     }
-    for (; c < c1; c += L * E) {
-        if (c + E <= c1) {
-            const Piece<T, E> x = Piece<T, E>::load(z + c);
-            take(x.x, c, E);
-        } else {
-            T x[E];
-#pragma unroll
-            for (int k = 0; k < E; ++k) x[k] = z[c + k < c1 ? c + k : c1 - 1];
-            take(x, c, c1 - c);
-        }
-    }
-    v = join_lanes<L>(v);
-    if (L == 256) {
-        if (threadIdx.x % 64 == 0) wave_sum[wave] = v;
-        __syncthreads();
-        v = wave_sum[0];
-        for (int w = 1; w < 4; ++w) v.join(wave_sum[w]);
-    }
-    const bool whole = L < 256 || a.parts == 1;
-    const float log_s = logf(v.s);
-    if (live && lane == 0) {
-        if (!whole) a.part_sum[unit] = v;
-        else finish_row(a, row, v, log_s, z);
-    }
-    if constexpr (R > 0) {
-        int mine = 0;                          // drawn from this lane
-        for (int k = 0; k < a.top; ++k) {
-            Rank r = max_over_lanes<L>(best.head());
-            if (L == 256) {
-                if (threadIdx.x % 64 == 0) wave_top[k & 1][wave] = r;
-                __syncthreads();
-                r = wave_top[k & 1][0];
-                for (int w = 1; w < 4; ++w) r = wave_top[k & 1][w] > r ? wave_top[k & 1][w] : r;
-            }
-            if (live && lane == 0) {
-                if (!whole) a.part_top[unit * a.top + k] = r;
-                else {
-                    a.top_idx[row * a.top + k] = rank_class(r);
-                    a.top_logp[row * a.top + k] = v.log_p(order_value((unsigned)(r >> 32)), log_s);
-                }
-            }
-            if (r != 0 && best.head() == r) {
-                best.pop();
-                if (++mine % R == 0 && k + 1 < a.top) {
-                    for (int cc = c0 + lane * E; cc < c1; cc += L * E)
-                        for (int e = 0; e < E && cc + e < c1; ++e) {
-                            const unsigned key = order_key(to_f32(z[cc + e]));
-                            if (rank_of(key, cc + e) < r) best.see(key, cc + e);
-                        }
-                }
+}
+
+// The alternatives, one after the other: each the highest head of all lanes' lists.  A lane whose list was drawn empty goes over its classes again for those
+// behind the last one drawn: rare (more than R of a row's highest in one lane) and exact.  draw(r): the highest rank of all lanes.
+template <class T, int L, int R, class Draw, class Put>
+__device__ __forceinline__ void draw_alternatives(Highest<R> &best, int top, const T *z, int c0, int c1, int lane, Draw draw, Put put) {
+    constexpr int E = kPerPiece<T>;
+    int mine = 0;                          // drawn from this lane
+    for (int k = 0; k < top; ++k) {
+        const Rank r = draw(best.head(), k);
+        put(r, k);
+        if (r != 0 && best.head() == r) {
+            best.pop();
+            if (++mine % R == 0 && k + 1 < top) {
+                for (int cc = c0 + lane * E; cc < c1; cc += L * E)
+                    for (int e = 0; e < E && cc + e < c1; ++e) {
+                        const unsigned key = order_key(to_f32(z[cc + e]));
+                        if (rank_of(key, cc + e) < r) best.see(key, cc + e);
+                    }
             }
         }
     }
 }
 
+// Rows that L lanes (4, 16, 64) hold in their registers, PIECES 16-byte pieces a lane: the maximum first, then one sum.
+template <class T, int L, int PIECES, int R>
+__global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
+    constexpr int E = kPerPiece<T>;
+    const int lane = threadIdx.x % L;
+    const long long row = a.row0 + (long long)blockIdx.x * (kLogThreads / L) + threadIdx.x / L;
+    const bool live = row < a.rows;      // whole groups of lanes; nobody leaves before the lanes' exchanges
+    const T *z = static_cast<const T *>(a.Z) + (live ? row : a.rows - 1) * a.ld;
+    Piece<T, E> x[PIECES];
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+        const int c = (q * L + lane) * E;
+        if (c + E <= a.classes) x[q] = Piece<T, E>::load(z + c);
+        else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) x[q].x[k] = c + k < a.classes ? z[c + k] : from_f32<T>(-INFINITY);
+        }
+    }
+    RowSum v = RowSum::empty();
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q)
+#pragma unroll
+        for (int k = 0; k < E; ++k) v.m = fmaxf(v.m, to_f32(x[q].x[k]));
+    v.m = max_over<L>(v.m);
+    const RowBase base(v.m);
+    Highest<R> best;
+    best.clear();
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+        const int c = (q * L + lane) * E;
+        if (q > 0 && q * L * E >= a.classes) break;      // the same in every lane
+        float f[E];
+#pragma unroll
+        for (int k = 0; k < E; ++k) f[k] = to_f32(x[q].x[k]);
+        add_powers<T, E>(v, base, f);
+        if (R > 0) {
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (c + k < a.classes) best.see(order_key(f[k]), c + k);
+        }
+    }
+    v.s = sum_over<L>(v.s);
+    v.t = sum_over<L>(v.t);
+    const float log_s = v.log_sum();
+    if (live && lane == 0) finish_row(a, row, v, log_s, z);
+    if constexpr (R > 0)
+        draw_alternatives<T, L, R>(best, a.top, z, 0, a.classes, lane, [&](Rank r, int) { return max_over_lanes<L>(r); }, [&](Rank r, int k) {
+            if (live && lane == 0) {
+                a.top_idx[row * a.top + k] = rank_class(r);
+                a.top_logp[row * a.top + k] = v.log_p(order_value((unsigned)(r >> 32)), log_s);
+            }
+        });
+}
+
+// Long rows, a workgroup each or (parts) several: one pass with a running maximum, m raised to m' multiplies s by f = exp(m - m') and turns t into
+// (t + (m - m') s) f.  R: classes that a lane keeps for the alternatives (0: none asked for).  A wavefront now and then raises the bar for
+// all its lanes to the a.top-th highest of their best: a class that is not above it has that many before it (all of lower numbers),
+// so that most classes are looked at no further than their step's maximum.
+template <class T, int R>
+__global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
+    constexpr int E = kPerPiece<T>, U = 4, L = kLogThreads;
+    __shared__ RowSum wave_sum[4];
+    __shared__ Rank wave_top[2][4];
+    const int lane = threadIdx.x, wave = threadIdx.x / 64;
+    const long long unit = (long long)blockIdx.x, row = a.row0 + unit / a.parts;
+    const int c0 = (int)(unit % a.parts) * a.part_classes, c1 = c0 + a.part_classes < a.classes ? c0 + a.part_classes : a.classes;
+    const T *z = static_cast<const T *>(a.Z) + row * a.ld;
+    RowSum v = RowSum::empty();
+    Highest<R> best;
+    best.clear();
+    float bar = NAN;
+    auto take = [&](const Piece<T, E> &x, int c, int n) {   // n classes from c on, n <= E
+        float f[E], top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            f[k] = k < n ? to_f32(x.x[k]) : -INFINITY;
+            top = fmaxf(top, f[k]);
+        }
+        if (top > v.m) v.raise(top);
+        add_powers<T, E>(v, RowBase(v.m), f);
+        if constexpr (R > 0) {
+            if (!(top <= bar) || v.s != v.s) {   // NaN is above all, and once there shows in the sum
+#pragma unroll
+                for (int k = 0; k < E; ++k)
+                    if (k < n && !(f[k] <= bar)) {
+                        best.see(order_key(f[k]), c + k);
+                        const float least = best.least();
+                        if (least == least && !(bar >= least)) bar = least;     // NaN while the list has room and no bar was raised
+                    }
+            }
+        }
+    };
+    int c = c0 + lane * E, step = 0, next = 1;
+    for (; c + (U - 1) * L * E + E <= c1; c += U * L * E) {
+        Piece<T, E> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = Piece<T, E>::load(z + c + u * L * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) take(x[u], c + u * L * E, E);
+        if constexpr (R > 0) {
+            if (++step == next) {
+                next *= 2;
+                if (__popcll(__ballot(1)) == 64) {      // the bits of the a.top-th highest (at most one a lane), from the highest on
+                    unsigned at = 0;
+                    const unsigned head = best.key[0];
+#pragma unroll
+                    for (int bit = 31; bit >= 0; --bit) {
+                        const unsigned with = at | 1u << bit;
+                        if (__popcll(__ballot(head >= with)) >= a.top) at = with;
+                    }
+                    if (at != 0u && at != 0xFFFFFFFFu) {
+                        const float raised = order_value(at);
+                        if (!(raised <= bar)) bar = raised;
+                    }
+                }
+            }
+        }
+    }
+    for (; c < c1; c += L * E) {
+        Piece<T, E> x;
+        if (c + E <= c1) x = Piece<T, E>::load(z + c);
+        else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) x.x[k] = z[c + k < c1 ? c + k : c1 - 1];
+        }
+        take(x, c, c1 - c < E ? c1 - c : E);
+    }
+    const float most = max_over<64>(v.m);
+    if (most > v.m) v.raise(most);
+    v.s = sum_over<64>(v.s);
+    v.t = sum_over<64>(v.t);
+    if (threadIdx.x % 64 == 0) wave_sum[wave] = v;
+    __syncthreads();
+    v = wave_sum[0];
+    for (int w = 1; w < 4; ++w) v.join(wave_sum[w]);
+    const float log_s = v.log_sum();
+    if (lane == 0) {
+        if (a.parts > 1) a.part_sum[unit] = v;
+        else finish_row(a, row, v, log_s, z);
+    }
+    if constexpr (R > 0)
+        draw_alternatives<T, L, R>(best, a.top, z, c0, c1, lane,
+            [&](Rank r, int k) {
+                r = max_over_lanes<64>(r);
+                if (threadIdx.x % 64 == 0) wave_top[k & 1][wave] = r;
+                __syncthreads();
+                r = wave_top[k & 1][0];
+                for (int w = 1; w < 4; ++w) r = wave_top[k & 1][w] > r ? wave_top[k & 1][w] : r;
+                return r;
+            },
+            [&](Rank r, int k) {
+                if (lane != 0) return;
+                if (a.parts > 1) a.part_top[unit * a.top + k] = r;
+                else {
+                    a.top_idx[row * a.top + k] = rank_class(r);
+                    a.top_logp[row * a.top + k] = v.log_p(order_value((unsigned)(r >> 32)), log_s);
+                }
+            });
+}
+
 // Joins what the parts of long rows left: a wavefront a row.
 template <class T> __global__ __launch_bounds__(64) void k_logprobs_join(LogArgs a) {
+    __shared__ Rank lists[kMaxParts * SENSEI_MAX_TOP];
     const long long row = blockIdx.x;
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x, n = a.parts * a.top;
+    for (int k = lane; k < n; k += 64) lists[k] = a.part_top[row * n + k];
     RowSum v = RowSum::empty();
     if (lane < a.parts) v = a.part_sum[row * a.parts + lane];
-    v = join_lanes<64>(v);
-    const float log_s = logf(v.s);
+    const float most = max_over<64>(v.m);
+    if (most > v.m) v.raise(most);
+    v.s = sum_over<64>(v.s);
+    v.t = sum_over<64>(v.t);
+    const float log_s = v.log_sum();
     if (lane == 0) finish_row(a, row, v, log_s, static_cast<const T *>(a.Z) + row * a.ld);
+    __syncthreads();
     int next = 0;
-    const Rank *list = a.part_top + (row * a.parts + lane) * a.top;
+    const Rank *list = lists + lane * a.top;
     Rank head = a.top > 0 && lane < a.parts ? list[0] : 0;
     for (int k = 0; k < a.top; ++k) {
         const Rank r = max_over_lanes<64>(head);
@@ -368,14 +473,27 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_backward(LogArgs a) {
     const int y = a.g_logp ? a.labels[row] : -1;
     const bool has = y >= 0 && y < a.classes;
     const float2 st = a.stats[row];
-    const float g = has ? a.g_logp[row] : 0.f, h = a.g_entropy ? a.g_entropy[row] : 0.f, ent = a.g_entropy ? a.entropy_in[row] : 0.f;
+    const float g = has ? a.g_logp[row] : 0.f, h = a.g_entropy ? a.g_entropy[row] : 0.f;
+    const RowBase base(st.x);
+    // exp(z - m) as the forward forms it, times what is the same for the row: 1 / s, and -g where there is no entropy term
+    const float inv_s = st.y == -INFINITY ? 0.f : expf(-base.shift() - st.y), by_g = -g * inv_s, at_max = -g - h * ((a.g_entropy ? a.entropy_in[row] : 0.f) - st.y);
+    auto one = [&](float f) {
+        const float e = base.power(f);
+        if (!a.g_entropy) return e * by_g;
+        return e == 0.f ? 0.f : e * inv_s * fmaf(-h, f - base.m, at_max);   // -g - h (log p + entropy)
+    };
     const bool empty = st.y == -INFINITY;
-    auto one = [&](float f, int c) {
-        const float lp = (f - st.x) - st.y, p = empty ? 0.f : exp_neg(lp);
-        float d = -g * p;
-        if (a.g_entropy) d = fmaf(-h * p, fmaxf(lp, -FLT_MAX) + ent, d);
-        if (p == 0.f) d = 0.f;
-        return has && c == y ? d + g : d;
+    auto piece = [&](Piece<T, E> &x, int c) {
+        float f[E];
+#pragma unroll
+        for (int k = 0; k < E; ++k) f[k] = empty ? 0.f : one(to_f32(x.x[k]));
+        if (has && y >= c && y < c + E) {
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (c + k == y) f[k] += g;
+        }
+#pragma unroll
+        for (int k = 0; k < E; ++k) x.x[k] = from_f32<T>(f[k]);
     };
     int c = c0 + lane * E;
     for (; c + (U - 1) * L * E + E <= c1; c += U * L * E) {
@@ -384,24 +502,28 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_backward(LogArgs a) {
         for (int u = 0; u < U; ++u) x[u] = Piece<T, E>::load(z + c + u * L * E);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int k = 0; k < E; ++k) x[u].x[k] = from_f32<T>(one(to_f32(x[u].x[k]), c + u * L * E + k));
+            piece(x[u], c + u * L * E);
             x[u].store(dz + c + u * L * E);
         }
     }
     for (; c < c1; c += L * E) {
         if (c + E <= c1) {
             Piece<T, E> x = Piece<T, E>::load(z + c);
-#pragma unroll
-            for (int k = 0; k < E; ++k) x.x[k] = from_f32<T>(one(to_f32(x.x[k]), c + k));
+            piece(x, c);
             x.store(dz + c);
         } else {
-            for (int k = c; k < c1; ++k) dz[k] = from_f32<T>(one(to_f32(z[k]), k));
+            Piece<T, E> x;
+#pragma unroll
+            for (int k = 0; k < E; ++k) x.x[k] = z[c + k < c1 ? c + k : c1 - 1];
+            piece(x, c);
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (c + k < c1) dz[c + k] = x.x[k];
         }
     }
 }
 
-// Lanes a row: the fewest that take it in eight steps at most.
+// Lanes a row: the fewest that hold it in two, four or eight pieces each.
 int log_lanes(int classes, int per_piece) {
     const int pieces = (classes + per_piece - 1) / per_piece;
     return pieces <= 8 ? 4 : pieces <= 64 ? 16 : pieces <= 512 ? 64 : 256;
@@ -419,10 +541,14 @@ template <class Launch> hipError_t by_rows(LogArgs a, int L, Launch launch) {
     return hipSuccess;
 }
 
+template <class T, int L, int R> void launch_log(const LogArgs &a, dim3 grid, hipStream_t s) {
+    if constexpr (L == 256) hipLaunchKernelGGL((k_logprobs_long<T, R>), grid, dim3(kLogThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_logprobs_short<T, L, L == 4 ? 2 : L == 16 ? 4 : 8, R>), grid, dim3(kLogThreads), 0, s, a);
+}
 template <class T, int L> void launch_log(const LogArgs &a, dim3 grid, hipStream_t s) {
-    if (a.top == 0) hipLaunchKernelGGL((k_logprobs<T, L, 0>), grid, dim3(kLogThreads), 0, s, a);
-    else if (a.top == 1) hipLaunchKernelGGL((k_logprobs<T, L, 1>), grid, dim3(kLogThreads), 0, s, a);
-    else hipLaunchKernelGGL((k_logprobs<T, L, 4>), grid, dim3(kLogThreads), 0, s, a);
+    if (a.top == 0) launch_log<T, L, 0>(a, grid, s);
+    else if (a.top == 1) launch_log<T, L, 1>(a, grid, s);
+    else launch_log<T, L, 4>(a, grid, s);
 }
 
 template <class T> hipError_t logprobs_typed(const LogArgs &args, hipStream_t s) {
@@ -453,12 +579,11 @@ template <class T> hipError_t logprobs_backward_typed(LogArgs args, hipStream_t 
     });
 }
 
-// Workgroups that share a row: where the rows alone leave the chip short of workgroups, as many as fill it (1,024) while a part keeps 8,192 classes.
+// Workgroups that share a row: where the rows alone leave the chip short of workgroups, as many as fill it (1,024) while a part keeps 2,048 classes.
 int log_parts(int64_t rows, int classes, int per_piece) {
     if (log_lanes(classes, per_piece) < 256 || rows >= 512) return 1;
-    int64_t parts = 1024 / rows, most = classes / 8192;
-    if (parts > most) parts = most;
-    return parts < 1 ? 1 : parts > 64 ? 64 : (int)parts;
+    const int64_t want = 1024 / rows, most = classes / 2048, parts = want < most ? want : most;
+    return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : (int)parts;
 }
 
 }  // namespace
