@@ -219,11 +219,19 @@ template <> struct Highest<0> {
     __device__ __forceinline__ void see(unsigned, int) {}
 };
 
+template <int CTRL> __device__ __forceinline__ Rank dpp_rank(Rank r) { return (Rank)(unsigned)dpp<CTRL>((int)(r >> 32)) << 32 | (unsigned)dpp<CTRL>((int)(unsigned)r); }
+__device__ __forceinline__ Rank higher(Rank a, Rank b) { return a > b ? a : b; }
+// the highest of L lanes' ranks, in all of them (as over_lanes)
 template <int L> __device__ __forceinline__ Rank max_over_lanes(Rank r) {
-#pragma unroll
-    for (int d = (L < 64 ? L : 64) / 2; d > 0; d >>= 1) {
-        const Rank o = __shfl_xor(r, d, 64);
-        r = o > r ? o : r;
+    r = higher(r, dpp_rank<0xB1>(r));
+    r = higher(r, dpp_rank<0x4E>(r));
+    if (L >= 16) {
+        r = higher(r, dpp_rank<0x141>(r));
+        r = higher(r, dpp_rank<0x140>(r));
+    }
+    if (L >= 64) {
+        r = higher(r, __shfl_xor(r, 16, 64));
+        r = higher(r, __shfl_xor(r, 32, 64));
     }
     return r;
 }
@@ -249,8 +257,9 @@ template <class T, int E> __device__ __forceinline__ void add_powers(RowSum &v, 
 
 // The alternatives, one after the other: each the highest head of all lanes' lists.  A lane whose list was drawn empty goes over its classes again for those
 // behind the last one drawn: rare (more than R of a row's highest in one lane) and exact.  draw(r): the highest rank of all lanes.
+// Classes [c0, c1), `head` single ones (one each of the first lanes) before those that the lanes take by pieces.
 template <class T, int L, int R, class Draw, class Put>
-__device__ __forceinline__ void draw_alternatives(Highest<R> &best, int top, const T *z, int c0, int c1, int lane, Draw draw, Put put) {
+__device__ __forceinline__ void draw_alternatives(Highest<R> &best, int top, const T *z, int c0, int head, int c1, int lane, Draw draw, Put put) {
     constexpr int E = kPerPiece<T>;
     int mine = 0;                          // drawn from this lane
     for (int k = 0; k < top; ++k) {
@@ -259,11 +268,13 @@ __device__ __forceinline__ void draw_alternatives(Highest<R> &best, int top, con
         if (r != 0 && best.head() == r) {
             best.pop();
             if (++mine % R == 0 && k + 1 < top) {
-                for (int cc = c0 + lane * E; cc < c1; cc += L * E)
-                    for (int e = 0; e < E && cc + e < c1; ++e) {
-                        const unsigned key = order_key(to_f32(z[cc + e]));
-                        if (rank_of(key, cc + e) < r) best.see(key, cc + e);
-                    }
+                auto again = [&](int c) {
+                    const unsigned key = order_key(to_f32(z[c]));
+                    if (rank_of(key, c) < r) best.see(key, c);
+                };
+                if (lane < head) again(c0 + lane);
+                for (int cc = c0 + head + lane * E; cc < c1; cc += L * E)
+                    for (int e = 0; e < E && cc + e < c1; ++e) again(cc + e);
             }
         }
     }
@@ -315,12 +326,19 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
     const float log_s = v.log_sum();
     if (live && lane == 0) finish_row(a, row, v, log_s, z);
     if constexpr (R > 0)
-        draw_alternatives<T, L, R>(best, a.top, z, 0, a.classes, lane, [&](Rank r, int) { return max_over_lanes<L>(r); }, [&](Rank r, int k) {
+        draw_alternatives<T, L, R>(best, a.top, z, 0, 0, a.classes, lane, [&](Rank r, int) { return max_over_lanes<L>(r); }, [&](Rank r, int k) {
             if (live && lane == 0) {
                 a.top_idx[row * a.top + k] = rank_class(r);
                 a.top_logp[row * a.top + k] = v.log_p(order_value((unsigned)(r >> 32)), log_s);
             }
         });
+}
+
+// Elements before the first 16-byte address, at most n: rows that begin elsewhere (odd numbers of 16-bit classes) are read and written a quarter
+// slower in pieces across those addresses.
+template <class T> __device__ __forceinline__ int elements_to_line(const T *p, int n) {
+    const int k = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (int)sizeof(T);
+    return k < n ? k : n;
 }
 
 // Long rows, a workgroup each or (parts) several: one pass with a running maximum, m raised to m' multiplies s by f = exp(m - m') and turns t into
@@ -361,7 +379,13 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
             }
         }
     };
-    int c = c0 + lane * E, step = 0, next = 1;
+    const int head = elements_to_line(z + c0, c1 - c0);
+    if (lane < head) {
+        Piece<T, E> x;
+        x.x[0] = z[c0 + lane];
+        take(x, c0 + lane, 1);
+    }
+    int c = c0 + head + lane * E, step = 0, next = 1;
     for (; c + (U - 1) * L * E + E <= c1; c += U * L * E) {
         Piece<T, E> x[U];
 #pragma unroll
@@ -410,7 +434,7 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
         else finish_row(a, row, v, log_s, z);
     }
     if constexpr (R > 0)
-        draw_alternatives<T, L, R>(best, a.top, z, c0, c1, lane,
+        draw_alternatives<T, L, R>(best, a.top, z, c0, head, c1, lane,
             [&](Rank r, int k) {
                 r = max_over_lanes<64>(r);
                 if (threadIdx.x % 64 == 0) wave_top[k & 1][wave] = r;
@@ -459,74 +483,116 @@ template <class T> __global__ __launch_bounds__(64) void k_logprobs_join(LogArgs
 
 // dZ_j = g ([j = label] - p_j) - h p_j (log p_j + entropy),  p_j = exp((z_j - m) - log s): g and h the gradients of the row's log probability and entropy.
 // Read once, written once; classes without a share (-inf) and rows of nothing else get 0 from both terms but the label's own.
-template <class T, int L>
-__global__ __launch_bounds__(kLogThreads) void k_logprobs_backward(LogArgs a) {
-    constexpr int E = kPerPiece<T>, U = 4;
-    const int lane = threadIdx.x % L;
-    const long long unit = (long long)blockIdx.x * (kLogThreads / L) + threadIdx.x / L;
-    const long long row = a.row0 + (L == 256 ? unit / a.parts : unit);
-    if (row >= a.rows) return;
-    const int c0 = L == 256 ? (int)(unit % a.parts) * a.part_classes : 0;
-    const int c1 = L == 256 && c0 + a.part_classes < a.classes ? c0 + a.part_classes : a.classes;
-    const T *z = static_cast<const T *>(a.Z) + row * a.ld;
-    T *dz = static_cast<T *>(a.dZ) + row * a.lddz;
-    const int y = a.g_logp ? a.labels[row] : -1;
-    const bool has = y >= 0 && y < a.classes;
-    const float2 st = a.stats[row];
-    const float g = has ? a.g_logp[row] : 0.f, h = a.g_entropy ? a.g_entropy[row] : 0.f;
-    const RowBase base(st.x);
-    // exp(z - m) as the forward forms it, times what is the same for the row: 1 / s, and -g where there is no entropy term
-    const float inv_s = st.y == -INFINITY ? 0.f : expf(-base.shift() - st.y), by_g = -g * inv_s, at_max = -g - h * ((a.g_entropy ? a.entropy_in[row] : 0.f) - st.y);
-    auto one = [&](float f) {
-        const float e = base.power(f);
-        if (!a.g_entropy) return e * by_g;
-        return e == 0.f ? 0.f : e * inv_s * fmaf(-h, f - base.m, at_max);   // -g - h (log p + entropy)
-    };
-    const bool empty = st.y == -INFINITY;
-    auto piece = [&](Piece<T, E> &x, int c) {
+template <class T> struct RowGradient {
+    RowBase base;
+    float inv_s, by_g, h, at_max, g;
+    int label;      // -1: none
+    bool entropy, empty;
+    __device__ __forceinline__ RowGradient(const LogArgs &a, long long row) : base(a.stats[row].x) {
+        const float log_s = a.stats[row].y;
+        label = a.g_logp ? a.labels[row] : -1;
+        if (label >= a.classes) label = -1;
+        g = label >= 0 ? a.g_logp[row] : 0.f;
+        entropy = a.g_entropy != nullptr;
+        h = entropy ? a.g_entropy[row] : 0.f;
+        empty = log_s == -INFINITY;
+        // a power times what is the same for the row: 1 / s, and -g where there is no entropy term
+        inv_s = empty ? 0.f : expf(-base.shift() - log_s);
+        by_g = -g * inv_s;
+        at_max = -g - h * ((entropy ? a.entropy_in[row] : 0.f) - log_s);
+    }
+    template <int E> __device__ __forceinline__ void piece(Piece<T, E> &x, int c) const {
         float f[E];
 #pragma unroll
-        for (int k = 0; k < E; ++k) f[k] = empty ? 0.f : one(to_f32(x.x[k]));
-        if (has && y >= c && y < c + E) {
+        for (int k = 0; k < E; ++k) {
+            const float z = to_f32(x.x[k]), e = base.power(z);
+            f[k] = !entropy ? e * by_g : e == 0.f ? 0.f : e * inv_s * fmaf(-h, z - base.m, at_max);   // -g - h (log p + entropy)
+            if (empty) f[k] = 0.f;
+        }
+        if (label >= c && label < c + E) {
 #pragma unroll
             for (int k = 0; k < E; ++k)
-                if (c + k == y) f[k] += g;
+                if (c + k == label) f[k] += g;
         }
 #pragma unroll
         for (int k = 0; k < E; ++k) x.x[k] = from_f32<T>(f[k]);
-    };
-    int c = c0 + lane * E;
+    }
+    // fewer than a piece
+    template <int E> __device__ __forceinline__ void some(const T *z, T *dz, int c, int n) const {
+        Piece<T, E> x;
+#pragma unroll
+        for (int k = 0; k < E; ++k) x.x[k] = z[c + (k < n ? k : 0)];
+        piece<E>(x, c);
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+            if (k < n) dz[c + k] = x.x[k];
+    }
+};
+
+template <class T, int L, int PIECES>
+__global__ __launch_bounds__(kLogThreads) void k_logprobs_backward_short(LogArgs a) {
+    constexpr int E = kPerPiece<T>;
+    const int lane = threadIdx.x % L;
+    const long long row = a.row0 + (long long)blockIdx.x * (kLogThreads / L) + threadIdx.x / L;
+    if (row >= a.rows) return;
+    const T *z = static_cast<const T *>(a.Z) + row * a.ld;
+    T *dz = static_cast<T *>(a.dZ) + row * a.lddz;
+    Piece<T, E> x[PIECES];
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+        const int c = (q * L + lane) * E;
+        if (c + E <= a.classes) x[q] = Piece<T, E>::load(z + c);
+    }
+    const RowGradient<T> grad(a, row);
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+        const int c = (q * L + lane) * E;
+        if (c + E <= a.classes) {
+            grad.template piece<E>(x[q], c);
+            x[q].store(dz + c);
+        } else if (c < a.classes) grad.template some<E>(z, dz, c, a.classes - c);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kLogThreads) void k_logprobs_backward_long(LogArgs a) {
+    constexpr int E = kPerPiece<T>, U = 4, L = kLogThreads;
+    const int lane = threadIdx.x;
+    const long long unit = (long long)blockIdx.x, row = a.row0 + unit / a.parts;
+    const int c0 = (int)(unit % a.parts) * a.part_classes, c1 = c0 + a.part_classes < a.classes ? c0 + a.part_classes : a.classes;
+    const T *z = static_cast<const T *>(a.Z) + row * a.ld;
+    T *dz = static_cast<T *>(a.dZ) + row * a.lddz;
+    const RowGradient<T> grad(a, row);
+    const int head = elements_to_line(dz + c0, c1 - c0);
+    if (lane < head) grad.template some<E>(z, dz, c0 + lane, 1);
+    int c = c0 + head + lane * E;
     for (; c + (U - 1) * L * E + E <= c1; c += U * L * E) {
         Piece<T, E> x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) x[u] = Piece<T, E>::load(z + c + u * L * E);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            piece(x[u], c + u * L * E);
+            grad.template piece<E>(x[u], c + u * L * E);
             x[u].store(dz + c + u * L * E);
         }
     }
     for (; c < c1; c += L * E) {
         if (c + E <= c1) {
             Piece<T, E> x = Piece<T, E>::load(z + c);
-            piece(x, c);
+            grad.template piece<E>(x, c);
             x.store(dz + c);
-        } else {
-            Piece<T, E> x;
-#pragma unroll
-            for (int k = 0; k < E; ++k) x.x[k] = z[c + k < c1 ? c + k : c1 - 1];
-            piece(x, c);
-#pragma unroll
-            for (int k = 0; k < E; ++k)
-                if (c + k < c1) dz[c + k] = x.x[k];
-        }
+        } else grad.template some<E>(z, dz, c, c1 - c);
     }
 }
 
-// Lanes a row: the fewest that hold it in two, four or eight pieces each.
-int log_lanes(int classes, int per_piece) {
-    const int pieces = (classes + per_piece - 1) / per_piece;
-    return pieces <= 8 ? 4 : pieces <= 64 ? 16 : pieces <= 512 ? 64 : 256;
+// Lanes a row and pieces a lane: eight pieces at most, on as few lanes as hold the row so (what is done once a row and lane is shared by more rows);
+// more than 64 lanes hold is walked.
+struct LogShape { int lanes, pieces; };
+LogShape log_shape(int classes, int per_piece) {
+    const int all = (classes + per_piece - 1) / per_piece;
+    LogShape s{all <= 32 ? 4 : all <= 128 ? 16 : all <= 512 ? 64 : 256, 1};
+    while (s.lanes < 256 && s.lanes * s.pieces < all) s.pieces *= 2;
+    return s;
 }
 
 // A launch has 2^22 workgroups at most (a grid's threads are counted in 32 bits): more rows than those take another one.
@@ -541,47 +607,41 @@ template <class Launch> hipError_t by_rows(LogArgs a, int L, Launch launch) {
     return hipSuccess;
 }
 
-template <class T, int L, int R> void launch_log(const LogArgs &a, dim3 grid, hipStream_t s) {
-    if constexpr (L == 256) hipLaunchKernelGGL((k_logprobs_long<T, R>), grid, dim3(kLogThreads), 0, s, a);
-    else hipLaunchKernelGGL((k_logprobs_short<T, L, L == 4 ? 2 : L == 16 ? 4 : 8, R>), grid, dim3(kLogThreads), 0, s, a);
+template <class T, int L, int PIECES> void launch_short(const LogArgs &a, bool backward, dim3 grid, hipStream_t s) {
+    const dim3 block(kLogThreads);
+    if (backward) hipLaunchKernelGGL((k_logprobs_backward_short<T, L, PIECES>), grid, block, 0, s, a);
+    else if (a.top == 0) hipLaunchKernelGGL((k_logprobs_short<T, L, PIECES, 0>), grid, block, 0, s, a);
+    else if (a.top == 1) hipLaunchKernelGGL((k_logprobs_short<T, L, PIECES, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_logprobs_short<T, L, PIECES, 4>), grid, block, 0, s, a);
 }
-template <class T, int L> void launch_log(const LogArgs &a, dim3 grid, hipStream_t s) {
-    if (a.top == 0) launch_log<T, L, 0>(a, grid, s);
-    else if (a.top == 1) launch_log<T, L, 1>(a, grid, s);
-    else launch_log<T, L, 4>(a, grid, s);
+template <class T> void launch_long(const LogArgs &a, bool backward, dim3 grid, hipStream_t s) {
+    const dim3 block(kLogThreads);
+    if (backward) hipLaunchKernelGGL(k_logprobs_backward_long<T>, grid, block, 0, s, a);
+    else if (a.top == 0) hipLaunchKernelGGL((k_logprobs_long<T, 0>), grid, block, 0, s, a);
+    else if (a.top == 1) hipLaunchKernelGGL((k_logprobs_long<T, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_logprobs_long<T, 4>), grid, block, 0, s, a);
 }
 
-template <class T> hipError_t logprobs_typed(const LogArgs &args, hipStream_t s) {
-    const int L = log_lanes(args.classes, kPerPiece<T>);
-    const hipError_t e = by_rows(args, L, [&](const LogArgs &a, dim3 grid) {
-        if (L == 4) launch_log<T, 4>(a, grid, s);
-        else if (L == 16) launch_log<T, 16>(a, grid, s);
-        else if (L == 64) launch_log<T, 64>(a, grid, s);
-        else launch_log<T, 256>(a, grid, s);
+template <class T> hipError_t logprobs_typed(const LogArgs &args, bool backward, hipStream_t s) {
+    const LogShape shape = log_shape(args.classes, kPerPiece<T>);
+    const hipError_t e = by_rows(args, shape.lanes, [&](const LogArgs &a, dim3 grid) {
+#define SENSEI_PIECES(L) \
+    (shape.pieces == 1 ? launch_short<T, L, 1>(a, backward, grid, s) : shape.pieces == 2 ? launch_short<T, L, 2>(a, backward, grid, s) \
+     : shape.pieces == 4 ? launch_short<T, L, 4>(a, backward, grid, s) : launch_short<T, L, 8>(a, backward, grid, s))
+        if (shape.lanes == 4) SENSEI_PIECES(4);
+        else if (shape.lanes == 16) SENSEI_PIECES(16);
+        else if (shape.lanes == 64) SENSEI_PIECES(64);
+        else launch_long<T>(a, backward, grid, s);
+#undef SENSEI_PIECES
     });
-    if (e != hipSuccess || args.parts == 1) return e;
+    if (e != hipSuccess || backward || args.parts == 1) return e;
     hipLaunchKernelGGL(k_logprobs_join<T>, dim3((unsigned)args.rows), dim3(64), 0, s, args);
     return hipGetLastError();
 }
 
-template <class T> hipError_t logprobs_backward_typed(LogArgs args, hipStream_t s) {
-    const int L = log_lanes(args.classes, kPerPiece<T>);
-    if (L == 256) {   // a workgroup takes 16,384 classes at most: long rows are shared, whatever their number
-        args.part_classes = 16384;
-        args.parts = (args.classes + args.part_classes - 1) / args.part_classes;
-    }
-    return by_rows(args, L, [&](const LogArgs &a, dim3 grid) {
-        const dim3 block(kLogThreads);
-        if (L == 4) hipLaunchKernelGGL((k_logprobs_backward<T, 4>), grid, block, 0, s, a);
-        else if (L == 16) hipLaunchKernelGGL((k_logprobs_backward<T, 16>), grid, block, 0, s, a);
-        else if (L == 64) hipLaunchKernelGGL((k_logprobs_backward<T, 64>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((k_logprobs_backward<T, 256>), grid, block, 0, s, a);
-    });
-}
-
 // Workgroups that share a row: where the rows alone leave the chip short of workgroups, as many as fill it (1,024) while a part keeps 2,048 classes.
 int log_parts(int64_t rows, int classes, int per_piece) {
-    if (log_lanes(classes, per_piece) < 256 || rows >= 512) return 1;
+    if (log_shape(classes, per_piece).lanes < 256 || rows >= 512) return 1;
     const int64_t want = 1024 / rows, most = classes / 2048, parts = want < most ? want : most;
     return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : (int)parts;
 }
@@ -623,9 +683,9 @@ hipError_t launch_logprobs(const sensei_tmat &Z, const int32_t *labels, int top,
         a.part_top = reinterpret_cast<Rank *>(static_cast<char *>(workspace) + align_up((size_t)Z.rows * a.parts * sizeof(RowSum), 256));
     }
     switch (Z.type) {
-    case SENSEI_F32: return logprobs_typed<float>(a, s);
-    case SENSEI_BF16: return logprobs_typed<Bf16>(a, s);
-    default: return logprobs_typed<F16>(a, s);
+    case SENSEI_F32: return logprobs_typed<float>(a, false, s);
+    case SENSEI_BF16: return logprobs_typed<Bf16>(a, false, s);
+    default: return logprobs_typed<F16>(a, false, s);
     }
 }
 
@@ -635,10 +695,14 @@ hipError_t launch_logprobs_backward(const sensei_tmat &Z, const int32_t *labels,
     LogArgs a = {};
     a.Z = Z.ptr; a.ld = Z.ld; a.rows = Z.rows; a.classes = (int)Z.cols; a.labels = labels; a.stats = const_cast<float2 *>(stats); a.g_logp = g_logp;
     a.entropy_in = entropy; a.g_entropy = g_entropy; a.dZ = dZ; a.lddz = lddz; a.parts = 1;
+    if (log_shape(a.classes, Z.type == SENSEI_F32 ? 4 : 8).lanes == 256) {   // a workgroup takes 16,384 classes at most: long rows are shared, whatever their number
+        a.part_classes = 16384;
+        a.parts = (a.classes + a.part_classes - 1) / a.part_classes;
+    }
     switch (Z.type) {
-    case SENSEI_F32: return logprobs_backward_typed<float>(a, s);
-    case SENSEI_BF16: return logprobs_backward_typed<Bf16>(a, s);
-    default: return logprobs_backward_typed<F16>(a, s);
+    case SENSEI_F32: return logprobs_typed<float>(a, true, s);
+    case SENSEI_BF16: return logprobs_typed<Bf16>(a, true, s);
+    default: return logprobs_typed<F16>(a, true, s);
     }
 }
 
