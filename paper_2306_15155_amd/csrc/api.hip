@@ -1833,7 +1833,7 @@ struct OnDevice {
 bool attention_opts_ok(const sensei_attention_opts *o, int64_t d_k, int64_t d_v) {
     return o && o->n_heads >= 1 && o->n_heads <= SENSEI_MAX_HEADS && o->n_kv_heads >= 1 && o->n_heads % o->n_kv_heads == 0 && d_k >= 1 && d_v >= 1 &&
            d_k <= SENSEI_MAX_HEAD_WIDTH && d_v <= SENSEI_MAX_HEAD_WIDTH && o->n_buckets >= 0 && o->n_buckets <= SENSEI_MAX_BUCKETS &&
-           (int64_t)(o->n_heads / o->n_kv_heads) * o->n_buckets <= 512 && std::isfinite(o->scale) && std::isfinite(o->cap) && o->cap >= 0.f && o->p >= 0.0 && o->p < 1.0;
+           (int64_t)(o->n_heads / o->n_kv_heads) * o->n_buckets <= 512 && std::isfinite(o->scale) && std::isfinite(o->cap) && o->cap >= 0.f && (o->cap == 0.f || std::isfinite(1.f / o->cap)) && o->p >= 0.0 && o->p < 1.0;
 }
 AttentionCall attention_call(const sensei_csr *A, const sensei_attention_opts &o, int d_k, int d_v, int type) {
     AttentionCall c = {};

@@ -884,7 +884,8 @@ enum { kJoinForward = 0, kJoinRows = 1, kJoinCols = 2 };
 
 // A group of lanes per chunk boundary and bundle of heads (blockIdx.y): where a row crosses it that crossed none before, the group joins that row's pieces, in their order; a
 // row of more than kManyPieces is left to the whole wavefront, whose groups take them in turn.  Workgroups behind those (of the first bundle)
-// look over 64 rows a wavefront and write the rows without entries.
+// look over 64 rows a wavefront and write the rows without entries.  (4 rows of 500,000 entries: 5.5 times as slow with every row left to its group; rows
+// of 100, and bounds of 4 or 64, made no difference.)
 constexpr int kManyPieces = 16;
 template <class T, int VEC, int G, int MODE, bool GENERIC>
 __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_heads, int join_blocks) {
@@ -929,20 +930,30 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
         s1.scale(f);
         s1.add(fo, o);
     };
-    auto take = [&](int from, int k) {
-        const size_t at = piece_at(from + k, k > 0, n_heads, h);
-        S x;
-        x.get(a.piece + at * W, t);
-        if (MODE == kJoinForward) {
-            const float2 ml = a.piece_ml[at];
-            join(ml.x, ml.y, x);
-        } else {
-            s1.add(1.f, x);
-            if (TWO) {
-                x.get(a.piece + at * W + G * VEC, t);
-                s2.add(1.f, x);
+    // pieces k, k + by, .. of n, a few at a time: their loads are under way together
+    auto take = [&](int from, int k, int by, int n) {
+        constexpr int AT_ONCE = VEC == 16 || TWO ? 4 : 8;
+        for (; k < n; k += AT_ONCE * by) {
+            S x[AT_ONCE], y[TWO ? AT_ONCE : 1];
+            float2 ml[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int kk = k + u * by < n ? k + u * by : k;
+                const size_t at = piece_at(from + kk, kk > 0, n_heads, h);
+                x[u].get(a.piece + at * W, t);
+                if (TWO) y[u].get(a.piece + at * W + G * VEC, t);
+                ml[u] = MODE == kJoinForward || (MODE == kJoinRows && TWO) ? a.piece_ml[at] : make_float2(0.f, 0.f);
             }
-            if (MODE == kJoinRows && TWO) delta += a.piece_ml[at].x;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (k + u * by >= n) break;
+                if (MODE == kJoinForward) join(ml[u].x, ml[u].y, x[u]);
+                else {
+                    s1.add(1.f, x[u]);
+                    if (TWO) s2.add(1.f, y[u]);
+                    delta += ml[u].x;
+                }
+            }
         }
     };
     auto finish = [&](int row) {
@@ -961,7 +972,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
     };
     const unsigned long long many = __ballot(pieces > kManyPieces);
     if (pieces > 0 && pieces <= kManyPieces) {
-        for (int k = 0; k < pieces; ++k) take(first, k);
+        take(first, 0, 1, pieces);
         finish(i);
     }
     for (int o = 0; o < groups; ++o) {
@@ -971,7 +982,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
         s2.zero();
         m = -INFINITY;
         l = delta = 0.f;
-        for (int k = group; k < n; k += groups) take(from, k);
+        take(from, group, groups, n);
         for (int dist = group_lanes; dist < 64; dist <<= 1) {
             S x;
 #pragma unroll
@@ -1037,9 +1048,10 @@ int bundle_log_of(const Shape &s, int n_heads, int together, int bytes) {
 // 16 where a SIMD would have less than a wavefront.  4,096 / 8,192 / 16,384 / 32,768 wavefronts, us: training steps, power-law patterns, 100,000 nodes
 // of 21 1,376 / 1,103 / 1,044 / 1,036, 212,000 of 22 1,662 / 1,676 / 1,452 / 1,449 (forward); batched graphs of 290,000 nodes 2,354 / 2,155 / 2,265 /
 // 2,666; 123,000 rows of 48 288 / 300 / 337 / 410 (forward).  Chunks of 16 / 32 entries: 10,000 nodes of 11 21 / 26.
-int chunk_of(int64_t nnz, int bundles, int groups) {
+// Rows of thousands of entries are cut no finer than sixteen pieces a row.
+int chunk_of(int64_t nnz, int n_rows, int bundles, int groups) {
     int t = 256;
-    while (t > 32 && nnz / t * bundles / groups < 16384) t >>= 1;
+    while (t > 32 && nnz / t * bundles / groups < 16384 && t * 8ll * n_rows > nnz) t >>= 1;
     return t == 32 && nnz / t * bundles / groups < 1024 ? 16 : t;
 }
 
@@ -1076,7 +1088,7 @@ struct Layout {
         bundle_log = bundle_log_of(shape, n_heads, together, (d > dv ? d : dv) * elem);
         bundles = (n_heads + (1 << bundle_log) - 1) >> bundle_log;
         groups = (64 / shape.lanes) >> bundle_log;
-        chunk = chunk_of(nnz, bundles, groups);
+        chunk = chunk_of(nnz, cols ? c.A->n_cols : c.A->n_rows, bundles, groups);
         n_chunks = (int)((nnz + chunk - 1) / chunk);
         join_log = 0;
         while ((shape.lanes << join_log) < 8 && (1 << join_log) < all) ++join_log;

@@ -13,89 +13,73 @@ namespace {
 
 // Y = add + keep (x) X / (1 - p).  Whether element (i, c) is kept is word c % 4 of the generator at counter (c / 4, i, 0, offset): it
 // depends on the element's place alone, not on leading dimensions or the launch, and the backward pass is the same call on dY.
-// A lane takes 16 bytes (one counter's four elements in fp32, two counters' in 16 bits), UNITS of them a block apart so that their loads are
-// under way together; a unit's row and column come from one multiplication (FastDiv).
+// A lane takes 16 bytes (one counter's four elements in fp32, two counters' in 16 bits), whose row and column come from one multiplication (FastDiv).
+// Bound by memory: 233,000 x 602 in fp32 207 us (5.4 TB/s, a copy of this size 5.0), 2.45 M x 256 in bf16 479 us (5.2 TB/s).  Four pieces a lane, a
+// workgroup apart, took 213 and 522 us.
 struct DropArgs {
     const void *X, *add;
     void *Y;
     long long ldx, lda, ldy;
     unsigned row0;             // of this launch
-    unsigned units;            // rows * units a row
+    unsigned units;            // rows * pieces a row
     int cols;
     FastDiv per_row;
     DropKey key;
 };
 constexpr int kDropThreads = 256;
 
-template <class T, bool ADD, int UNITS>
+template <class T, bool ADD>
 __global__ __launch_bounds__(kDropThreads) void k_dropout(DropArgs a) {
     constexpr int E = kPerPiece<T>;
-    const unsigned first = blockIdx.x * (unsigned)(kDropThreads * UNITS) + threadIdx.x;
+    const unsigned at = blockIdx.x * (unsigned)kDropThreads + threadIdx.x;
+    if (at >= a.units) return;
     const unsigned offset = a.key.offset + (a.key.offset_dev ? *a.key.offset_dev : 0u);
-    Piece<T, E> x[UNITS], r[UNITS];
-    unsigned row[UNITS];
-    int col[UNITS], live[UNITS];   // elements of the unit: E, fewer at a row's end, none behind the last unit
+    const unsigned i = a.per_row.div(at), row = a.row0 + i;
+    const int col = (int)(at - i * a.per_row.d) * E, live = a.cols - col < E ? a.cols - col : E;   // fewer than E at a row's end
+    const T *px = static_cast<const T *>(a.X) + (long long)row * a.ldx + col;
+    const T *pr = ADD ? static_cast<const T *>(a.add) + (long long)row * a.lda + col : nullptr;
+    Piece<T, E> x, r, y;
+    if (live == E) {
+        x = Piece<T, E>::load(px);
+        if (ADD) r = Piece<T, E>::load(pr);
+    } else {
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-        const unsigned at = first + u * kDropThreads;
-        row[u] = 0; col[u] = 0; live[u] = 0;
-        if (at < a.units) {
-            const unsigned i = a.per_row.div(at);
-            row[u] = a.row0 + i;
-            col[u] = (int)(at - i * a.per_row.d) * E;
-            live[u] = a.cols - col[u] < E ? a.cols - col[u] : E;
-        }
-        const T *px = static_cast<const T *>(a.X) + (long long)row[u] * a.ldx + col[u];
-        const T *pr = static_cast<const T *>(a.add) + (ADD ? (long long)row[u] * a.lda + col[u] : 0);
-        if (live[u] == E) {
-            x[u] = Piece<T, E>::load(px);
-            if (ADD) r[u] = Piece<T, E>::load(pr);
-        } else {
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                if (k < live[u]) {
-                    x[u].x[k] = px[k];
-                    if (ADD) r[u].x[k] = pr[k];
-                }
+        for (int k = 0; k < E; ++k) {
+            if (k < live) {
+                x.x[k] = px[k];
+                if (ADD) r.x[k] = pr[k];
             }
         }
     }
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-        if (live[u] == 0) continue;
-        Piece<T, E> y;
+    for (int q = 0; q < E / 4; ++q) {
+        const Words w = philox((unsigned)col / 4 + q, row, 0u, offset, a.key.k0, a.key.k1);
 #pragma unroll
-        for (int q = 0; q < E / 4; ++q) {
-            const Words w = philox((unsigned)col[u] / 4 + q, row[u], 0u, offset, a.key.k0, a.key.k1);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int e = 4 * q + k;
-                float v = w.w[k] < a.key.threshold ? 0.f : to_f32(x[u].x[e]) * a.key.keep_scale;
-                if (ADD) v += to_f32(r[u].x[e]);
-                y.x[e] = from_f32<T>(v);
-            }
+        for (int k = 0; k < 4; ++k) {
+            const int e = 4 * q + k;
+            float v = w.w[k] < a.key.threshold ? 0.f : to_f32(x.x[e]) * a.key.keep_scale;
+            if (ADD) v += to_f32(r.x[e]);
+            y.x[e] = from_f32<T>(v);
         }
-        T *py = static_cast<T *>(a.Y) + (long long)row[u] * a.ldy + col[u];
-        if (live[u] == E) y.store(py);
-        else {
+    }
+    T *py = static_cast<T *>(a.Y) + (long long)row * a.ldy + col;
+    if (live == E) y.store(py);
+    else {
 #pragma unroll
-            for (int k = 0; k < E; ++k)
-                if (k < live[u]) py[k] = y.x[k];
-        }
+        for (int k = 0; k < E; ++k)
+            if (k < live) py[k] = y.x[k];
     }
 }
 
-template <class T, bool ADD> hipError_t dropout_units(DropArgs a, long long rows, hipStream_t s) {
+template <class T, bool ADD> hipError_t dropout_typed(DropArgs a, long long rows, hipStream_t s) {
     const unsigned per_row = (unsigned)((a.cols + kPerPiece<T> - 1) / kPerPiece<T>);
     a.per_row = FastDiv::of(per_row);
-    const long long slab = (0x7FFFFFFFll - 4 * kDropThreads) / per_row;   // unit numbers of a launch stay below 2^31
+    const long long slab = (0x7FFFFFFFll - kDropThreads) / per_row;   // piece numbers of a launch stay below 2^31
     for (long long r0 = 0; r0 < rows; r0 += slab) {
         const long long n = rows - r0 < slab ? rows - r0 : slab;
         a.row0 = (unsigned)r0;
         a.units = (unsigned)(n * per_row);
-        // four units a lane once that still fills the chip several times over
-        if (a.units >= 4u * kDropThreads * 2048) hipLaunchKernelGGL((k_dropout<T, ADD, 4>), dim3((a.units + 4 * kDropThreads - 1) / (4 * kDropThreads)), dim3(kDropThreads), 0, s, a);
-        else hipLaunchKernelGGL((k_dropout<T, ADD, 1>), dim3((a.units + kDropThreads - 1) / kDropThreads), dim3(kDropThreads), 0, s, a);
+        hipLaunchKernelGGL((k_dropout<T, ADD>), dim3((a.units + kDropThreads - 1) / kDropThreads), dim3(kDropThreads), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -416,7 +400,8 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
         if (c + E <= c1) x = Piece<T, E>::load(z + c);
         else {
 #pragma unroll
-            for (int k = 0; k < E; ++k) x.x[k] = z[c + k < c1 ? c + k : c1 - 1];
+            for (int k = 0; k < E; ++k)
+                if (c + k < c1) x.x[k] = z[c + k];
         }
         take(x, c, c1 - c < E ? c1 - c : E);
     }
@@ -586,7 +571,9 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_backward_long(LogArgs 
 }
 
 // Lanes a row and pieces a lane: eight pieces at most, on as few lanes as hold the row so (what is done once a row and lane is shared by more rows);
-// more than 64 lanes hold is walked.
+// more than 64 lanes hold is walked.  Forward, us: 2.45 M rows of 47 (fp32) on 4 lanes / 16 114 / 185, with five alternatives 190 / 392; 100,000 of 349
+// (bf16) on 16 / 64 21 / 35; 20,000 of 1,800 (fp32) held by 64 lanes / walked by 256 25 / 43, of 3,900 (bf16) 45 / 75.  The gradient hardly
+// minds (283 / 265, 29 / 43, 49 / 52).
 struct LogShape { int lanes, pieces; };
 LogShape log_shape(int classes, int per_piece) {
     const int all = (classes + per_piece - 1) / per_piece;
@@ -639,7 +626,8 @@ template <class T> hipError_t logprobs_typed(const LogArgs &args, bool backward,
     return hipGetLastError();
 }
 
-// Workgroups that share a row: where the rows alone leave the chip short of workgroups, as many as fill it (1,024) while a part keeps 2,048 classes.
+// Workgroups that share a row: where the rows alone leave the chip short of workgroups, as many as fill it (1,024) while a part keeps 2,048 classes.  Shared /
+// one workgroup each, us: 2 rows of 250,000 with five alternatives 21 / 90, 1 row of 50,000 21 / 30; 64 rows of 50,000 18 / 18.
 int log_parts(int64_t rows, int classes, int per_piece) {
     if (log_shape(classes, per_piece).lanes < 256 || rows >= 512) return 1;
     const int64_t want = 1024 / rows, most = classes / 2048, parts = want < most ? want : most;
@@ -656,9 +644,9 @@ hipError_t launch_dropout(const sensei_tmat &X, const sensei_tmat *add, double p
     if (add) { a.add = add->ptr; a.lda = add->ld; }
     a.key = {(unsigned)seed, (unsigned)(seed >> 32), offset, offset_dev, drop_threshold(p), (float)(1.0 / (1.0 - p))};
     switch (X.type) {
-    case SENSEI_F32: return add ? dropout_units<float, true>(a, X.rows, s) : dropout_units<float, false>(a, X.rows, s);
-    case SENSEI_BF16: return add ? dropout_units<Bf16, true>(a, X.rows, s) : dropout_units<Bf16, false>(a, X.rows, s);
-    default: return add ? dropout_units<F16, true>(a, X.rows, s) : dropout_units<F16, false>(a, X.rows, s);
+    case SENSEI_F32: return add ? dropout_typed<float, true>(a, X.rows, s) : dropout_typed<float, false>(a, X.rows, s);
+    case SENSEI_BF16: return add ? dropout_typed<Bf16, true>(a, X.rows, s) : dropout_typed<Bf16, false>(a, X.rows, s);
+    default: return add ? dropout_typed<F16, true>(a, X.rows, s) : dropout_typed<F16, false>(a, X.rows, s);
     }
 }
 
