@@ -128,6 +128,60 @@ def test_head_layouts(ctx, heads, kv, d):
     Inputs(pattern("hub", heads), heads, kv, d, d, "f16", seed=heads).check(ctx, cap=3.0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("heads,kv,d,dv,buckets", [(4, 2, 96, 96, 5), (8, 2, 128, 40, 0), (6, 1, 72, 200, 3), (16, 1, 8, 8, 32), (64, 8, 8, 16, 64), (32, 2, 20, 33, 32), (4, 4, 5, 9, 128)])
+def test_shared_heads_and_bias_tables(ctx, heads, kv, d, dv, buckets, dtype):
+    """two query heads a lane (wide heads that share a key head), tables of the bias' gradient that ask for more lanes a head or smaller workgroups, masked buckets"""
+    x = Inputs(pattern("random", d), heads, kv, d, dv, dtype, buckets=buckets, seed=d, extra=(0, 8, 0, 3))
+    if buckets:
+        x.bias[1:, 1] = -np.inf
+    x.check(ctx, cap=6.0, p=0.3, seed=11)
+
+
+@pytest.mark.parametrize("n,ld", [(270, 4_200_000), (250, 4_000_000)])
+def test_rows_far_apart(ctx, n, ld):
+    """leading dimensions past 2^24 bytes and offsets past 2^32 in every matrix of the backward; the same just below both"""
+    rng = np.random.default_rng(1)
+    P = ref.Pattern(n, n, [np.append(rng.choice(n, 6, replace=False), n - 1) for _ in range(n)])
+    x = Inputs(P, 2, 1, 16, 16, "f32", seed=3)
+    for k in range(4):
+        buf = torch.empty(n * ld, device=DEV)
+        v = buf.view(n, ld)[:, 7: 7 + x.host[k].shape[1]]
+        v.copy_(x.host[k])
+        x.dev[k] = v
+    x.check(ctx, p=0.2)
+    x.dev = None
+
+
+def test_many_columns(ctx):
+    """column numbers past 2^24"""
+    m = 2 ** 24 + 100
+    rng = np.random.default_rng(2)
+    P = ref.Pattern(30, m, [np.unique(np.concatenate([rng.integers(0, m, 20), [m - 1 - i]])) for i in range(30)])
+    x = Inputs(P, 1, 1, 4, 4, "f32", seed=5)
+    want, got = x.want(grad=False), x.got(ctx, grad=True)
+    for k in ("Y", "stats"):
+        within(got[k], want[k], want["err"][k], k)
+    hit = torch.zeros(m, dtype=torch.bool, device=DEV)
+    hit[torch.from_numpy(P.col).to(DEV)] = True
+    assert torch.all(got["dK"][~hit] == 0) and torch.all(got["dV"][~hit] == 0) and torch.all(got["dV"][hit].abs().sum(1) > 0)
+
+
+def test_calls_on_two_streams_at_once(ctx):
+    x, y = Inputs(pattern("hub", 5), 4, 2, 16, 16, "f32", buckets=5, seed=6), Inputs(pattern("hub", 6), 4, 2, 16, 16, "f32", buckets=5, seed=7)
+    want = [v.got(ctx, p=0.4, seed=1) for v in (x, y)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [None, None]
+    for _ in range(5):
+        for k, v in enumerate((x, y)):
+            with torch.cuda.stream(streams[k]):
+                got[k] = v.got(ctx, p=0.4, seed=1)
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(want[k][n], got[k][n]) for n in want[k])
+
+
 def test_masked_entries_have_no_share(ctx):
     """bias of -inf hides infinities and NaN in keys and values, also where it leaves a row nothing; the type's lowest value does not"""
     P = pattern("random", 9)

@@ -108,7 +108,7 @@ def check_logprobs(ctx, z, Z, labels, top, dtype, grad=True):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("rows,classes,top", [(1, 1, 1), (5, 2, 2), (7, 3, 0), (300, 41, 5), (33, 47, 47), (1000, 8, 1), (64, 64, 64), (3, 65, 7), (17, 300, 10),
-                                              (9, 2047, 20), (4, 4099, 64), (600, 5001, 3)])
+                                              (9, 2047, 20), (4, 4099, 64), (600, 5001, 3), (70, 127, 12), (70, 129, 12), (41, 511, 9), (41, 513, 9), (11, 1025, 33)])
 def test_logprobs(ctx, dtype, rows, classes, top):
     z = normal(rows + classes, dtype, rows, classes, std=2.0)
     rng = np.random.default_rng(classes)
@@ -196,6 +196,17 @@ def test_wrong_arguments_raise(ctx):
     with pytest.raises(SenseiError):
         ctx.dropout(Z, 0.5, 1, add=Z.bfloat16())
     assert ctx.dropout(Z[:0], 0.5, 1).shape == (0, 5) and ctx.logprobs(Z[:0], lab[:0], top=2).top_idx.shape == (0, 2)
+
+
+def test_offsets_past_32_bits(ctx):
+    ld = 600_000_000
+    buf = torch.empty(3 * ld, dtype=torch.float16, device=DEV)
+    Z = buf.view(3, ld)[:, 11: 11 + 5000]
+    z = normal(9, "f16", 3, 5000)
+    Z.copy_(z)
+    check_logprobs(ctx, z, Z, np.array([5, 4999, -1]), 4, "f16")
+    want, err = ref.dropout(z, 0.3, 8, 2)
+    within(ctx.dropout(Z, 0.3, 8, 2, out=Z), want, err + HALF["f16"] * np.abs(want) * 1.01 + TINY["f16"], "dropout")
 
 
 def test_captured_and_replayed(ctx):

@@ -154,8 +154,8 @@ def test_attention_refuses():
     n = ctypes.c_size_t()
     q = lambda o, d=16, dv=16, type=0, a=A: L.sensei_attention_workspace(ctypes.byref(a), ctypes.byref(o), d, dv, type, ctypes.byref(n))  # noqa: E731
     assert q(opts()) == 0 and n.value > 0
-    for bad in (dict(n_heads=0), dict(n_kv_heads=3), dict(n_kv_heads=0), dict(n_heads=514), dict(cap=-1.0), dict(cap=float("inf")), dict(scale=float("nan")),
-                dict(n_buckets=129), dict(n_buckets=-1), dict(n_heads=128, n_buckets=65), dict(p=1.0), dict(p=-1e-9), dict(p=float("nan"))):
+    for bad in (dict(n_heads=0), dict(n_kv_heads=3), dict(n_kv_heads=0), dict(n_heads=514), dict(cap=-1.0), dict(cap=float("inf")), dict(cap=1e-45), dict(scale=float("nan")),
+                dict(n_buckets=129), dict(n_buckets=-1), dict(n_heads=32, n_buckets=33), dict(p=1.0), dict(p=-1e-9), dict(p=float("nan"))):
         assert q(opts(**bad)) == 1, bad
     assert q(opts(), d=0) == 1 and q(opts(), d=257) == 1 and q(opts(), dv=0) == 1 and q(opts(), type=3) == 1 and q(opts(), a=binding.CsrStruct(-1, 5, 0, 0x1000)) == 1
     base = dict(A=A, Q=mat(0x1000000, 100, 64), K=mat(0x2000000, 120, 32), V=mat(0x3000000, 120, 48), o=opts(), Y=0x4000000, ldy=96, stats=0x5000000, ws=0x60000000,
