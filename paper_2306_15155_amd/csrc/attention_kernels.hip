@@ -5,10 +5,11 @@
 // weights again from the rows' (m, log l):
 //     x = bias + cap tanh(scale <q, k> / cap),  p = exp(x - m - log l),  dt = p (keep/(1-p_drop) <dy, v> - D),  D_i = <dy_i, y_i>,
 //     dq_i = sum_j ds k_j,  dk_j = sum_i ds q_i,  dv_j = sum_i p keep/(1-p_drop) dy_i,  dbias[h, b] = sum dt,  ds = dt (1 - tanh^2) scale
-// as two walks, one over the rows (dq, dbias) and one over the transposed pattern (dk, dv), so that no sum needs an atomic.
+// as two walks, one over the rows (dq) and one over the transposed pattern (dk, dv, dbias), so that no sum needs an atomic across wavefronts.
 //
-// D comes from Y; where Y was rounded to 16 bits, what the rounding took from D is summed along (delta) and taken out of dq at the row's end,
-// and dbias is summed by the walk over the columns, which has the whole D.
+// D comes from Y.  Where Y was rounded to 16 bits, the walk over the rows sums what the rounding took from D along (delta = sum dt, 0 with the whole D)
+// and takes it out of dq at the row's end; dbias is summed by the walk over the columns, which has the whole D.  (Without: dbias 1.9e-3 of
+// its size off, the other gradients 10 % further than their own rounding.)
 //
 // What bounds these walks is the gathering of k and v (q and dy) rows from the caches, and behind it the instructions around four operations an
 // element.  A head's vector is spread over as few lanes as hold 32 bytes of it each (G: one lane for 16 elements of 16 bits); a group of lanes takes
@@ -126,7 +127,7 @@ __device__ __forceinline__ int here(int x) {
 // whose they are: every gather is a full piece within its row.  GENERIC (vectors shorter than a piece, matrices past 32-bit offsets): elements one by
 // one where a piece is not whole, 64-bit offsets.
 template <class T, int VEC, int G, bool GENERIC> struct Lanes {
-    static constexpr int PER = VEC < kPerPiece<T> ? VEC : kPerPiece<T>, PIECES = VEC / PER;
+    static constexpr int PER = kPerPiece<T>, PIECES = VEC / PER;
     __device__ __forceinline__ static int at(int r, int t) { return (r * G + t) * PER; }
     __device__ __forceinline__ static int from(int r, int t, int d) { return GENERIC || at(r, t) + PER <= d ? at(r, t) : d - PER; }
 };
@@ -180,23 +181,28 @@ template <class T, int VEC, int G, bool GENERIC> struct Source {
     }
     // `more`: bytes that are the same in every lane
     __device__ __forceinline__ Gathered<T, VEC> row(int i, long long more = 0) const {
+        using Raw = typename Piece<T, L::PER>::Raw;
         Gathered<T, VEC> x;
 #pragma unroll
         for (int r = 0; r < L::PIECES; ++r) {
-            if constexpr (!GENERIC) {
-                *reinterpret_cast<Piece<T, L::PER> *>(x.w + r * (L::PER * (int)sizeof(T) / 4)) =
-                    Piece<T, L::PER>::load(reinterpret_cast<const T *>((base + more) + (__umul24((unsigned)i, ld24) + offset[r])));
-            } else {
+            U32x4 raw;
+            if constexpr (!GENERIC) raw = *reinterpret_cast<const Raw *>((base + more) + (__umul24((unsigned)i, ld24) + offset[r]));
+            else {
                 const T *p = reinterpret_cast<const T *>(base + more + (long long)i * ld + offset[r]);
                 const int left = d - L::at(r, t);
                 Piece<T, L::PER> y;
                 if (left >= L::PER) y = Piece<T, L::PER>::load(p);
                 else {
 #pragma unroll
-                    for (int k = 0; k < L::PER; ++k) y.x[k] = k < left ? p[k] : T{};
+                    for (int k = 0; k < L::PER; ++k) {
+                        y.x[k] = T{};
+                        if (k < left) y.x[k] = p[k];
+                    }
                 }
-                *reinterpret_cast<Piece<T, L::PER> *>(x.w + r * (L::PER * (int)sizeof(T) / 4)) = y;
+                raw = __builtin_bit_cast(U32x4, y);
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x.w[4 * r + k] = raw[k];
         }
         return x;
     }
@@ -288,7 +294,8 @@ struct Walk {
     unsigned bucket;         // four of eight bits
     __device__ __forceinline__ void fetch(const WalkPattern &p, int at) {
         if (at + kBatch <= p.nnz) {
-            const Piece<float, 4>::Raw x = *reinterpret_cast<const Piece<float, 4>::Raw *>(p.col + at);
+            typedef U32x4 Four __attribute__((aligned(4)));
+            const U32x4 x = *reinterpret_cast<const Four *>(p.col + at);
             col[0] = (int)x.x; col[1] = (int)x.y; col[2] = (int)x.z; col[3] = (int)x.w;
             typedef unsigned Byte4 __attribute__((aligned(1)));
             bucket = p.bucket ? *reinterpret_cast<const Byte4 *>(p.bucket + at) : 0u;
@@ -302,7 +309,7 @@ struct Walk {
             }
         }
     }
-    __device__ __forceinline__ void look_ahead(const WalkPattern &p) { next_end = p.row_ptr[i + 2 < p.n_rows ? i + 2 : p.n_rows]; }
+    __device__ __forceinline__ void look_ahead(const WalkPattern &p) { next_end = p.row_ptr[i < p.n_rows - 2 ? i + 2 : p.n_rows]; }
     // The row of the chunk's first entry is found by the group's lanes together (lane `j` of `lanes`), which narrow the rows down (4 lanes + 1)-fold a
     // look: a launch that did so ahead of the walk cost 9 us.
     __device__ __forceinline__ void begin(const WalkPattern &p, int chunk, int j, int lanes) {
@@ -312,7 +319,7 @@ struct Walk {
         int lo = 0, hi = p.n_rows;     // row_ptr[lo] <= e < row_ptr[hi]
         const unsigned long long mine = (lanes < 64 ? (1ull << lanes) - 1 : ~0ull) << ((int)(threadIdx.x & 63) - j);
         while (hi - lo > 1) {
-            const int step = (hi - lo + 4 * lanes) / (4 * lanes + 1);
+            const int step = (hi - lo - 1) / (4 * lanes + 1) + 1;
             int below = 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -320,7 +327,7 @@ struct Walk {
                 below += __popcll(__ballot(at < hi && p.row_ptr[at < hi ? at : lo] <= e) & mine);
             }
             lo += step * below;
-            if (lo + step < hi) hi = lo + step;
+            if (step < hi - lo) hi = lo + step;
         }
         i = lo;
         row_end = p.row_ptr[i + 1];
@@ -351,8 +358,8 @@ struct Walk {
             int lo = i, hi = i, step = 1;
             do {
                 lo = hi;
-                hi = hi + step < p.n_rows ? hi + step : p.n_rows - 1;
-                step *= 2;
+                hi = step < p.n_rows - hi ? hi + step : p.n_rows - 1;
+                step = step < 1 << 29 ? 2 * step : step;
             } while (p.row_ptr[hi + 1] <= e);
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;

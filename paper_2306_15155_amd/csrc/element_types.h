@@ -21,12 +21,10 @@ template <> __device__ __forceinline__ F16 from_f32<F16>(float x) { return {__bu
 
 // N elements side by side.  The hardware takes wide global accesses at any address, so an odd leading dimension or head width costs no
 // other path; the vector types say what alignment there is.
-typedef unsigned U32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned U32x4 __attribute__((ext_vector_type(4)));
 template <int BYTES, int ALIGN> struct RawOf;
 template <> struct RawOf<16, 4> { typedef U32x4 type __attribute__((aligned(4))); };
 template <> struct RawOf<16, 2> { typedef U32x4 type __attribute__((aligned(2))); };
-template <> struct RawOf<8, 2> { typedef U32x2 type __attribute__((aligned(2))); };
 
 template <class T, int N> struct Piece {
     typedef typename RawOf<N * (int)sizeof(T), (int)sizeof(T)>::type Raw;
