@@ -373,7 +373,10 @@ struct Walk {
     }
 };
 
-// Where a lane works: t of the G lanes of head h, group `chunk` of the walk.  The lanes of a bundle's heads that there are not work along on the last
+// Where a lane works: t of the G lanes of head h, group `chunk` of the walk.  The first workgroups take the last chunks: where node numbers follow
+// degrees from the highest down (power-law patterns mostly do), those are the chunks of many short rows, which take longest and would run on
+// alone at the end (first / last chunks first, us: training steps, 100,000 nodes of 21 1,108 / 959, 97,000 of 11 994 / 893, forward, 233,000 of 87
+// 1,965 / 1,733; uniform patterns alike, 2,210 / 2,196, 614 / 611).  The lanes of a bundle's heads that there are not work along on the last
 // head (others want what they work out) and store nothing.
 template <int G> struct Place {
     int t, slot, in_bundle, h, chunk;
@@ -387,7 +390,7 @@ template <int G> struct Place {
         in_group = lane & (group_lanes - 1);
         in_bundle = slot & ((1 << bundle_log) - 1);
         const int head = ((int)blockIdx.y << bundle_log) + in_bundle;
-        chunk = ((int)blockIdx.x * waves() + (int)(threadIdx.x >> 6)) * groups + (slot >> bundle_log);
+        chunk = ((int)(gridDim.x - 1 - blockIdx.x) * waves() + (int)(threadIdx.x >> 6)) * groups + (slot >> bundle_log);
         live = chunk < n_chunks;
         head_live = head < n_heads;
         h = head_live ? head : n_heads - 1;
@@ -1051,14 +1054,15 @@ int bundle_log_of(const Shape &s, int n_heads, int together, int bytes) {
     while ((s.lanes << (log + 1)) <= 64 && (1 << log) < n_heads && ((bytes << log) / together < 256 || (1 << log) < together)) ++log;
     return log;
 }
-// Entries of a chunk: as many as leave 16,384 wavefronts, 32 to 256, so that chunks of many short rows (a batch each, however few their entries) even out;
-// 16 where a SIMD would have less than a wavefront.  4,096 / 8,192 / 16,384 / 32,768 wavefronts, us: training steps, power-law patterns, 100,000 nodes
-// of 21 1,376 / 1,103 / 1,044 / 1,036, 212,000 of 22 1,662 / 1,676 / 1,452 / 1,449 (forward); batched graphs of 290,000 nodes 2,354 / 2,155 / 2,265 /
-// 2,666; 123,000 rows of 48 288 / 300 / 337 / 410 (forward).  Chunks of 16 / 32 entries: 10,000 nodes of 11 21 / 26.
+// Entries of a chunk: as many as leave 8,192 wavefronts, 32 to 256, so that chunks of many short rows (a batch each, however few their entries) even out
+// and pieces of rows stay few; 16 where a SIMD would have less than a wavefront.  4,096 / 8,192 / 16,384 wavefronts, us: power-law patterns, training,
+// 100,000 nodes of 21 1,273 / 959 / 933, 97,000 of 11 1,065 / 893 / 866, forward, 212,000 of 22 1,542 / 1,552 / 1,366; uniform ones, training, batched
+// graphs of 290,000 nodes 2,405 / 2,196 / 2,279, 51,000 rows of 60 1,555 / 1,639 / 1,743, forward, 123,000 rows of 48 306 / 308 / 339, 172,000 of 16
+// 631 / 611 / 654.  Chunks of 16 / 32 entries: 10,000 nodes of 11 21 / 26.
 // Rows of thousands of entries are cut no finer than sixteen pieces a row.
 int chunk_of(int64_t nnz, int n_rows, int bundles, int groups) {
     int t = 256;
-    while (t > 32 && nnz / t * bundles / groups < 16384 && t * 8ll * n_rows > nnz) t >>= 1;
+    while (t > 32 && nnz / t * bundles / groups < 8192 && t * 8ll * n_rows > nnz) t >>= 1;
     return t == 32 && nnz / t * bundles / groups < 1024 ? 16 : t;
 }
 
