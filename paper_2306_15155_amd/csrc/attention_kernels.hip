@@ -18,6 +18,8 @@
 // the lanes of a head share them out: cap, bias, mask and exponential are worked out once an entry and head, and the weights are handed
 // round by moves within a quad of lanes; so are the generator's words, of which a call has four heads'.  Rows that cross chunks leave a
 // piece per chunk in scratch, joined by a second kernel in chunk order: results do not depend on scheduling.
+#include <algorithm>
+
 #include "element_types.h"
 #include "sensei_internal.h"
 
@@ -293,7 +295,7 @@ struct Walk {
     int col[kBatch];
     unsigned bucket;         // four of eight bits
     __device__ __forceinline__ void fetch(const WalkPattern &p, int at) {
-        if (at + kBatch <= p.nnz) {
+        if (at <= p.nnz - kBatch) {
             typedef U32x4 Four __attribute__((aligned(4)));
             const U32x4 x = *reinterpret_cast<const Four *>(p.col + at);
             col[0] = (int)x.x; col[1] = (int)x.y; col[2] = (int)x.z; col[3] = (int)x.w;
@@ -1021,17 +1023,18 @@ __global__ __launch_bounds__(kThreads) void k_attention_row_stats(AttnArgs a, un
         if (k < nnz) out[t_pos[k]] = bucket[k];
         return;
     }
-    const long long at = (long long)blockIdx.x * (kThreads / G) + threadIdx.x / G;
-    if (at >= (long long)a.p.n_rows * a.heads) return;
-    const int i = (int)(at / a.heads), h = (int)(at % a.heads), t = threadIdx.x % G;
-    const Source<T, VEC, G, GENERIC> Y(a.Y, a.ldy, h * a.dv, a.dv, t), dY(a.dY, a.lddy, h * a.dv, a.dv, t);
-    const Gathered<T, VEC> y = Y.own(i), dy = dY.own(i);
-    const float2 ml = a.stats[at];
-    float d = 0.f;
+    const int t = threadIdx.x % G;
+    for (long long at = (long long)blockIdx.x * (kThreads / G) + threadIdx.x / G; at < (long long)a.p.n_rows * a.heads; at += (long long)blocks * (kThreads / G)) {
+        const int i = (int)(at / a.heads), h = (int)(at % a.heads);
+        const Source<T, VEC, G, GENERIC> Y(a.Y, a.ldy, h * a.dv, a.dv, t), dY(a.dY, a.lddy, h * a.dv, a.dv, t);
+        const Gathered<T, VEC> y = Y.own(i), dy = dY.own(i);
+        const float2 ml = a.stats[at];
+        float d = 0.f;
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) d = fmaf(dy.get(k), y.get(k), d);
-    d = sum_over<G>(d);
-    if (t == 0) a.row_stats[at] = make_float4(ml.x, ml.y, d, 0.f);
+        for (int k = 0; k < VEC; ++k) d = fmaf(dy.get(k), y.get(k), d);
+        d = sum_over<G>(d);
+        if (t == 0) a.row_stats[at] = make_float4(ml.x, ml.y, d, 0.f);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------------------------ host side
@@ -1184,7 +1187,8 @@ template <class T, int VEC, int G, bool GENERIC> hipError_t rows_shape(const Att
     a.O1 = c.dQ; a.ldo1 = c.lddq;
     a.bundle_log = l.bundle_log;
     if (a.p.nnz > 0) {
-        const unsigned blocks = (unsigned)(((int64_t)a.p.n_rows * a.heads + kThreads / G - 1) / (kThreads / G)), more = a.bias ? (unsigned)((a.p.nnz + kThreads - 1) / kThreads) : 0;
+        // 2^22 workgroups at most (a grid's threads are counted in 32 bits): more rows and heads than those take another turn
+        const unsigned blocks = (unsigned)std::min<int64_t>(((int64_t)a.p.n_rows * a.heads + kThreads / G - 1) / (kThreads / G), 1 << 22), more = a.bias ? (unsigned)((a.p.nnz + kThreads - 1) / kThreads) : 0;
         hipLaunchKernelGGL((k_attention_row_stats<T, VEC, G, GENERIC>), dim3(blocks + more), dim3(kThreads), 0, s, a, blocks, c.bucket, c.t_pos, a.p.nnz, bucket_t);
         const dim3 grid(l.blocks(kThreads / 64), l.bundles), block(kThreads);
         if constexpr (!GENERIC && kShaped<T, VEC, 2>) {
