@@ -14,7 +14,7 @@ namespace {
 // Y = add + keep (x) X / (1 - p).  Whether element (i, c) is kept is word c % 4 of the generator at counter (c / 4, i, 0, offset): it
 // depends on the element's place alone, not on leading dimensions or the launch, and the backward pass is the same call on dY.
 // A lane takes 16 bytes (one counter's four elements in fp32, two counters' in 16 bits), whose row and column come from one multiplication (FastDiv).
-// Bound by memory: 233,000 x 602 in fp32 207 us (5.4 TB/s, a copy of this size 5.0), 2.45 M x 256 in bf16 479 us (5.2 TB/s).  Four pieces a lane, a
+// Bound by memory: 233,000 x 602 in fp32 207 us (5.4 TB/s, a copy of this size 5.0), 2.45 M x 256 in bf16 462 us (5.4 TB/s), with a residual 622 us (6.0).  Four pieces a lane, a
 // workgroup apart, took 213 and 522 us.
 struct DropArgs {
     const void *X, *add;
@@ -264,7 +264,8 @@ __device__ __forceinline__ void draw_alternatives(Highest<R> &best, int top, con
     }
 }
 
-// Rows that L lanes (4, 16, 64) hold in their registers, PIECES 16-byte pieces a lane: the maximum first, then one sum.
+// Rows that L lanes (4, 16, 64) hold in their registers, PIECES 16-byte pieces a lane: the maximum first, then one sum.  Bound by memory once there are
+// rows enough: 233,000 x 41 in fp32 10 us (3.9 TB/s), the gradient 21 us (3.6 TB/s); 1,024 x 47 is the launch.
 template <class T, int L, int PIECES, int R>
 __global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
     constexpr int E = kPerPiece<T>;
@@ -328,7 +329,8 @@ template <class T> __device__ __forceinline__ int elements_to_line(const T *p, i
 // Long rows, a workgroup each or (parts) several: one pass with a running maximum, m raised to m' multiplies s by f = exp(m - m') and turns t into
 // (t + (m - m') s) f.  R: classes that a lane keeps for the alternatives (0: none asked for).  A wavefront now and then raises the bar for
 // all its lanes to the a.top-th highest of their best: a class that is not above it has that many before it (all of lower numbers),
-// so that most classes are looked at no further than their step's maximum.
+// so that most classes are looked at no further than their step's maximum.  Bound by memory: 16,384 x 50,021 in fp16 343 us (4.8 TB/s), the gradient
+// 637 us (5.1 TB/s); with ten alternatives in bf16 the vector instructions weigh as much: 4,096 x 100,003 205 to 240 us (3.4 to 4.0 TB/s).
 template <class T, int R>
 __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
     constexpr int E = kPerPiece<T>, U = 4, L = kLogThreads;
