@@ -560,12 +560,12 @@ __global__ __launch_bounds__(kThreads) void k_attention(AttnArgs a) {
                 const float y = score_of(a, x[o]).x + b[r][o];
                 x[o] = use[o] ? y : -INFINITY;
             }
-            const float top = fmaxf(m[r], O::max(x)), base = top > -INFINITY ? top : 0.f, f = exp_neg(m[r] - base);
+            const float top = fmaxf(m[r], O::max(x)), base = top > -INFINITY ? top : 0.f, f = exp_weight(m[r] - base);
             m[r] = top;
             l[r] *= f;
 #pragma unroll
             for (int o = 0; o < O::N; ++o) {
-                const float p = exp_neg(x[o] - base);
+                const float p = exp_weight(x[o] - base);
                 l[r] += p;
                 x[o] = a.key.threshold && !(keep[o] >> r & 1) ? 0.f : p;
             }
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_rows(AttnArgs a) {
             for (int o = 0; o < O::N; ++o) {
                 const Score sc = score_of(a, x[o]);
                 const float dp = a.key.threshold && !(keep[o] >> r & 1) ? 0.f : dv[o] * a.key.keep_scale;
-                const float p = use[o] ? exp_neg((sc.x + b[r][o] - st[r].x) - st[r].y) : 0.f, dt = use[o] ? p * (dp - st[r].z) : 0.f, by = sc.slope * a.scale;
+                const float p = use[o] ? exp_weight((sc.x + b[r][o] - st[r].x) - st[r].y) : 0.f, dt = use[o] ? p * (dp - st[r].z) : 0.f, by = sc.slope * a.scale;
                 delta[r] += dt;
                 x[o] = dt * by;
                 pb[o] = use[o] ? p * by : 0.f;
@@ -826,7 +826,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_back_cols(AttnArgs a) {
                 for (int o = 0; o < O::N; ++o) {
                     const Score sc = score_of(a, x[o]);
                     const float ks = a.key.threshold && !(keep[o] & 1) ? 0.f : a.key.keep_scale, dp = ks == 0.f ? 0.f : pw[o] * ks;
-                    const float p = use[o] ? exp_neg((sc.x + b[o] - st[o].x) - st[o].y) : 0.f, dt = use[o] ? p * (dp - st[o].z) : 0.f;
+                    const float p = use[o] ? exp_weight((sc.x + b[o] - st[o].x) - st[o].y) : 0.f, dt = use[o] ? p * (dp - st[o].z) : 0.f;
                     x[o] = dt * sc.slope * a.scale;
                     pw[o] = p * ks;
                     if (a.bias_part) {   // a head's lanes one after the other: two may be in one bucket
@@ -943,7 +943,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_join(AttnArgs a, int n_h
     s2.zero();
     float m = -INFINITY, l = 0.f, delta = 0.f;
     auto join = [&](float om, float ol, const S &o) {
-        const float top = fmaxf(m, om), base = top > -INFINITY ? top : 0.f, f = exp_neg(m - base), fo = exp_neg(om - base);
+        const float top = fmaxf(m, om), base = top > -INFINITY ? top : 0.f, f = exp_weight(m - base), fo = exp_weight(om - base);
         m = top;
         l = l * f + ol * fo;
         s1.scale(f);

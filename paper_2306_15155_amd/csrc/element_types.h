@@ -38,6 +38,10 @@ constexpr float kLog2E = 1.44269502162933349609375f;        // log2(e) rounded t
 constexpr float kLog2ELow = 1.92596303380834e-8f;           // ... and what the rounding left
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// exp(x) by one product and one instruction: off by |x| 2^-24 of itself for the product's rounding, beside the instruction's unit in the last place.  For a
+// softmax, whose sums weigh that with exp(x): 2^-24 / e of the largest at most.  0 for -inf, NaN stays NaN.
+__device__ __forceinline__ float exp_weight(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+
 // exp(x) for x <= 0 (a little above is fine): 2^(x log2 e) with the product's rounding put back to first order, so that the error stays at the
 // exponential instruction's own unit in the last place however large |x| is.  Below -104 the result is under the smallest fp32 number
 // of any kind: zero.  NaN stays NaN.

@@ -90,33 +90,32 @@ template <class T, bool ADD> hipError_t dropout_typed(DropArgs a, long long rows
 
 // One row of C logits z: with its maximum m,
 //     s = sum exp(z - m),  t = sum (z - m) exp(z - m);   lse = m + log s,  entropy = log s - t / s,  log p_j = (z_j - m) - log s.
-// Classes at -inf have no share (and add 0 to t); a row of nothing else has lse = -inf.  The exponential of an element is one fused product and one
-// instruction: exp(z - m) = 2^(z L - c) 2^(c - m L), L = log2(e) in fp32, c = m L rounded: the second factor, the same for a whole row, is put right in
-// log s.  Where m L has no room in fp32 (rows of a type's lowest value) the difference is formed first.
+// Classes at -inf have no share (and add 0 to t); a row of nothing else has lse = -inf.
+//
+// The gradient needs no difference of its own: exp(z - m) = 2^(z L - c) 2^(c - m L), L = log2(e) in fp32, c = m L rounded, is one fused product and one
+// instruction an element, and the second factor, the same for a whole row, goes with 1 / s.  Where m L has no room in fp32 (rows of a type's lowest
+// value) the difference is formed first.
 struct RowBase {
-    float m, c;      // c finite, or -inf: differences
-    bool direct;
+    float m, c;
+    bool direct;     // differences
     __device__ __forceinline__ explicit RowBase(float top) {
 #pragma clang fp contract(off)   // c is the rounded product wherever it goes
         m = top > -INFINITY ? top : 0.f;
         direct = !(fabsf(m) < 1e30f);      // and an infinite maximum, whose row is NaN whatever is done
         c = direct ? 0.f : m * kLog2E;
     }
-    __device__ __forceinline__ float power(float z) const { return direct ? exp_neg(z - m) : __builtin_amdgcn_exp2f(fmaf(z, kLog2E, -c)); }
-    // log of a power over that of exp(z - m); log of a sum of powers as if they were exp(z - m)
+    template <bool DIRECT> __device__ __forceinline__ float power(float z) const { return DIRECT ? exp_neg(z - m) : __builtin_amdgcn_exp2f(fmaf(z, kLog2E, -c)); }
+    // log of a power over that of exp(z - m)
     __device__ __forceinline__ float shift() const { return direct ? 0.f : fmaf(m, kLog2E, -c) * kLn2; }
-    __device__ __forceinline__ float log_sum(float s) const { return logf(s) - shift(); }
 };
 
 // Sums of a part of a row whose maximum is known to be at least every element of it.
 struct RowSum {
-    float m, s, t;   // powers relative to m
+    float m, s, t;   // relative to m
     __device__ __forceinline__ static RowSum empty() { return {-INFINITY, 0.f, 0.f}; }
     __device__ __forceinline__ void raise(float top) {   // top > m
         if (m > -INFINITY) {
-            const RowBase old(m), now(top);
-            // powers of the old base to those of the new one
-            const float f = old.direct || now.direct ? exp_neg(m - top) : __builtin_amdgcn_exp2f(old.c - now.c);
+            const float f = exp_neg(m - top);
             t = f == 0.f ? 0.f : fmaf(m - top, s, t) * f;   // the difference may be as low as a type's lowest value
             s *= f;
         }
@@ -129,7 +128,6 @@ struct RowSum {
         s += b.s;
         t += b.t;
     }
-    __device__ __forceinline__ float log_sum() const { return RowBase(m).log_sum(s); }
     // z - lse, the large numbers first: exact where m is far from 0 (a row of nothing but a type's lowest value)
     __device__ __forceinline__ float log_p(float z, float log_s) const { return s == 0.f ? -INFINITY : (z - m) - log_s; }
 };
@@ -229,13 +227,14 @@ template <class T> __device__ __forceinline__ void finish_row(const LogArgs &a, 
     }
 }
 
-// E classes side by side into the sums (relative to base, which is at least their maximum)
-template <class T, int E> __device__ __forceinline__ void add_powers(RowSum &v, const RowBase &base, const float (&f)[E]) {
+// E classes side by side into the sums (whose m is at least their maximum)
+template <int E> __device__ __forceinline__ void add_powers(RowSum &v, const float (&f)[E]) {
+    const float base = v.m > -INFINITY ? v.m : 0.f;
 #pragma unroll
     for (int k = 0; k < E; ++k) {
-        const float e = base.power(f[k]);
+        const float d = f[k] - base, e = exp_weight(d);
         v.s += e;
-        v.t = fmaf(e, fmaxf(f[k] - base.m, -FLT_MAX), v.t);   // -inf: 0 times a finite number
+        v.t = fmaf(e, fmaxf(d, -FLT_MAX), v.t);   // -inf: 0 times a finite number
     }
 }
 
@@ -265,7 +264,7 @@ __device__ __forceinline__ void draw_alternatives(Highest<R> &best, int top, con
 }
 
 // Rows that L lanes (4, 16, 64) hold in their registers, PIECES 16-byte pieces a lane: the maximum first, then one sum.  Bound by memory once there are
-// rows enough: 233,000 x 41 in fp32 10 us (3.9 TB/s), the gradient 21 us (3.6 TB/s); 1,024 x 47 is the launch.
+// rows enough: 233,000 x 41 in fp32 10 us (3.9 TB/s), the gradient 18 us (4.2 TB/s); 1,024 x 47 is the launch.
 template <class T, int L, int PIECES, int R>
 __global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
     constexpr int E = kPerPiece<T>;
@@ -289,7 +288,6 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
 #pragma unroll
         for (int k = 0; k < E; ++k) v.m = fmaxf(v.m, to_f32(x[q].x[k]));
     v.m = max_over<L>(v.m);
-    const RowBase base(v.m);
     Highest<R> best;
     best.clear();
 #pragma unroll
@@ -299,7 +297,7 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
         float f[E];
 #pragma unroll
         for (int k = 0; k < E; ++k) f[k] = to_f32(x[q].x[k]);
-        add_powers<T, E>(v, base, f);
+        add_powers(v, f);
         if (R > 0) {
 #pragma unroll
             for (int k = 0; k < E; ++k)
@@ -308,7 +306,7 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_short(LogArgs a) {
     }
     v.s = sum_over<L>(v.s);
     v.t = sum_over<L>(v.t);
-    const float log_s = v.log_sum();
+    const float log_s = logf(v.s);
     if (live && lane == 0) finish_row(a, row, v, log_s, z);
     if constexpr (R > 0)
         draw_alternatives<T, L, R>(best, a.top, z, 0, 0, a.classes, lane, [&](Rank r, int) { return max_over_lanes<L>(r); }, [&](Rank r, int k) {
@@ -330,7 +328,8 @@ template <class T> __device__ __forceinline__ int elements_to_line(const T *p, i
 // (t + (m - m') s) f.  R: classes that a lane keeps for the alternatives (0: none asked for).  A wavefront now and then raises the bar for
 // all its lanes to the a.top-th highest of their best: a class that is not above it has that many before it (all of lower numbers),
 // so that most classes are looked at no further than their step's maximum.  Bound by memory: 16,384 x 50,021 in fp16 343 us (4.8 TB/s), the gradient
-// 637 us (5.1 TB/s); with ten alternatives in bf16 the vector instructions weigh as much: 4,096 x 100,003 205 to 240 us (3.4 to 4.0 TB/s).
+// 637 us (5.1 TB/s); with ten alternatives in bf16 the vector instructions weigh as much: 4,096 x 100,003 209 us (3.9 TB/s; with the
+// exponential's argument chosen element by element 226).
 template <class T, int R>
 __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
     constexpr int E = kPerPiece<T>, U = 4, L = kLogThreads;
@@ -352,7 +351,7 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
             top = fmaxf(top, f[k]);
         }
         if (top > v.m) v.raise(top);
-        add_powers<T, E>(v, RowBase(v.m), f);
+        add_powers(v, f);
         if constexpr (R > 0) {
             if (!(top <= bar) || v.s != v.s) {   // NaN is above all, and once there shows in the sum
 #pragma unroll
@@ -415,7 +414,7 @@ __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
     __syncthreads();
     v = wave_sum[0];
     for (int w = 1; w < 4; ++w) v.join(wave_sum[w]);
-    const float log_s = v.log_sum();
+    const float log_s = logf(v.s);
     if (lane == 0) {
         if (a.parts > 1) a.part_sum[unit] = v;
         else finish_row(a, row, v, log_s, z);
@@ -452,7 +451,7 @@ template <class T> __global__ __launch_bounds__(64) void k_logprobs_join(LogArgs
     if (most > v.m) v.raise(most);
     v.s = sum_over<64>(v.s);
     v.t = sum_over<64>(v.t);
-    const float log_s = v.log_sum();
+    const float log_s = logf(v.s);
     if (lane == 0) finish_row(a, row, v, log_s, static_cast<const T *>(a.Z) + row * a.ld);
     __syncthreads();
     int next = 0;
@@ -474,7 +473,7 @@ template <class T> struct RowGradient {
     RowBase base;
     float inv_s, by_g, h, at_max, g;
     int label;      // -1: none
-    bool entropy, empty;
+    bool entropy;
     __device__ __forceinline__ RowGradient(const LogArgs &a, long long row) : base(a.stats[row].x) {
         const float log_s = a.stats[row].y;
         label = a.g_logp ? a.labels[row] : -1;
@@ -482,20 +481,27 @@ template <class T> struct RowGradient {
         g = label >= 0 ? a.g_logp[row] : 0.f;
         entropy = a.g_entropy != nullptr;
         h = entropy ? a.g_entropy[row] : 0.f;
-        empty = log_s == -INFINITY;
+        const bool empty = log_s == -INFINITY;     // its powers are all 0
         // a power times what is the same for the row: 1 / s, and -g where there is no entropy term
         inv_s = empty ? 0.f : expf(-base.shift() - log_s);
-        by_g = -g * inv_s;
+        by_g = empty ? 0.f : -g * inv_s;
         at_max = -g - h * ((entropy ? a.entropy_in[row] : 0.f) - log_s);
+    }
+    template <bool DIRECT, int E> __device__ __forceinline__ void terms(const Piece<T, E> &x, float (&f)[E]) const {
+#pragma unroll
+        for (int k = 0; k < E; ++k) f[k] = base.template power<DIRECT>(to_f32(x.x[k]));
+        if (entropy) {
+#pragma unroll
+            for (int k = 0; k < E; ++k) f[k] = f[k] == 0.f ? 0.f : f[k] * inv_s * fmaf(-h, to_f32(x.x[k]) - base.m, at_max);   // -g - h (log p + entropy)
+        } else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) f[k] *= by_g;
+        }
     }
     template <int E> __device__ __forceinline__ void piece(Piece<T, E> &x, int c) const {
         float f[E];
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-            const float z = to_f32(x.x[k]), e = base.power(z);
-            f[k] = !entropy ? e * by_g : e == 0.f ? 0.f : e * inv_s * fmaf(-h, z - base.m, at_max);   // -g - h (log p + entropy)
-            if (empty) f[k] = 0.f;
-        }
+        if (base.direct) terms<true, E>(x, f);     // once a piece, not once an element
+        else terms<false, E>(x, f);
         if (label >= c && label < c + E) {
 #pragma unroll
             for (int k = 0; k < E; ++k)
