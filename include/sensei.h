@@ -506,7 +506,7 @@ int sensei_dropout(sensei_ctx *ctx, sensei_tmat X, const sensei_tmat *add, doubl
  * distance or the direction, sampled neighbours are a rectangular one.  bucket: nnz bytes (device, in the pattern's order) that sort the
  * entries by distance or kind (a number from n_buckets on counts as the last bucket), bias: n_heads x n_buckets floats (device); n_buckets = 0: no
  * bias, both ignored.  bias may be -inf: such entries are masked and have no share, whatever Q, K or V hold; K and V of other entries enter as
- * they are (a NaN there comes out in the rows that attend to it, an infinity as the formulas have it: a score of -inf has no share, +inf makes NaN).  drop: alpha_ij keep / (1 - p), the softmax's sum over all
+ * they are (a NaN there comes out in the rows that attend to it, an infinity does as NaN, as an infinity or as no share).  drop: alpha_ij keep / (1 - p), the softmax's sum over all
  * entries; the weight of entry (i, j) and query head h is kept if word h % 4 of the generator of sensei_dropout at counter
  * (j, i, 2^31 + h / 4, offset [+ *offset_dev]) is at least p 2^32: the mask does not depend on the order of the entries.
  * A row with no entry, or with masked ones only, has Y = 0 and the pair (-inf, -inf).

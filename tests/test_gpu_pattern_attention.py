@@ -1,5 +1,7 @@
 """Attention over a pattern and its gradients on the GPU against the definition in 64 bits: head layouts and widths, types, rows from no entry to
 thousands, masks, strides, dropped weights, capture."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -333,3 +335,27 @@ def test_training_step_of_all_of_them(ctx):
         torch.cuda.synchronize()
         for u, v in zip(out, step(20 + k)):
             assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("d", [16, 25])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_infinite_keys(ctx, dtype, d):
+    """rows that do not attend to an infinite key keep theirs; where vectors are whole pieces a score of -inf has no share, one of +inf makes NaN"""
+    P = pattern("random", 4)
+    x = Inputs(P, 2, 2, d, d, dtype, seed=7)
+    j = int(P.col[0])
+    rows = torch.zeros(P.n_rows, dtype=torch.bool)
+    rows[torch.from_numpy(P.row[P.col == j])] = True
+    rows = rows.to(DEV)
+    x.dev[0].abs_().add_(1)                       # products with a key of one sign have that sign
+    x.dev[1][j] = -60000.0
+    low = x.got(ctx, grad=False)["Y"]
+    for key in (-math.inf, math.inf):
+        x.dev[1][j] = key
+        Y = x.got(ctx, grad=False)["Y"]
+        assert torch.equal(Y[~rows], low[~rows])
+        if key > 0:
+            assert torch.isnan(Y[rows]).all()
+        elif d == 16:
+            several = rows & torch.from_numpy(np.diff(P.row_ptr) > 1).to(DEV)
+            assert several.any() and torch.equal(Y[several], low[several])
