@@ -20,9 +20,9 @@
 // piece per chunk in scratch, joined by a second kernel in chunk order: results do not depend on scheduling.
 //
 // Walks, us, and what they gather a second (every entry's vectors counted):             forward       over rows     over columns
-//     100,000 nodes of 21, 4 heads of 32, fp32, cap, bias, drop                         267, 8.1 TB/s 259, 8.3 TB/s 353, 6.5 TB/s
-//     290,000 nodes in graphs of 10 to 60, 8 heads of 16, bf16, bias, drop              533, 11 TB/s  707, 8.5 TB/s 861, 8.8 TB/s
-//     233,000 nodes of 87, 8 query on 2 key heads of 64, bf16, cap                      1,714, 6.0 TB/s
+//     100,000 nodes of 21, 4 heads of 32, fp32, cap, bias, drop                         262, 8.2 TB/s 259, 8.3 TB/s 354, 6.5 TB/s
+//     290,000 nodes in graphs of 10 to 60, 8 heads of 16, bf16, bias, drop              515, 12 TB/s  654, 9.2 TB/s 800, 9.4 TB/s
+//     233,000 nodes of 87, 8 query on 2 key heads of 64, bf16, cap                      1,650, 6.3 TB/s
 // In fp32 that is what lines from L2s and the Infinity Cache come at; in 16 bits half as many lines carry as many operations, and two thirds of
 // the time are vector instructions at two or three wavefronts a SIMD (132 to 250 registers).
 #include <algorithm>

@@ -327,9 +327,9 @@ template <class T> __device__ __forceinline__ int elements_to_line(const T *p, i
 // Long rows, a workgroup each or (parts) several: one pass with a running maximum, m raised to m' multiplies s by f = exp(m - m') and turns t into
 // (t + (m - m') s) f.  R: classes that a lane keeps for the alternatives (0: none asked for).  A wavefront now and then raises the bar for
 // all its lanes to the a.top-th highest of their best: a class that is not above it has that many before it (all of lower numbers),
-// so that most classes are looked at no further than their step's maximum.  Bound by memory: 16,384 x 50,021 in fp16 343 us (4.8 TB/s), the gradient
-// 637 us (5.1 TB/s); with ten alternatives in bf16 the vector instructions weigh as much: 4,096 x 100,003 209 us (3.9 TB/s; with the
-// exponential's argument chosen element by element 226).
+// so that most classes are looked at no further than their step's maximum.  Bound by memory: 16,384 x 50,021 in fp16 320 us (5.1 TB/s), the gradient
+// 637 us (5.1 TB/s); with ten alternatives in bf16 the vector instructions weigh as much: 4,096 x 100,003 187 to 211 us by card (3.9 to 4.4 TB/s; with the
+// exponential's argument chosen element by element 226 where this took 209).
 template <class T, int R>
 __global__ __launch_bounds__(kLogThreads) void k_logprobs_long(LogArgs a) {
     constexpr int E = kPerPiece<T>, U = 4, L = kLogThreads;
